@@ -71,7 +71,8 @@ typedef enum {
     CLEARMOE_ERR_WORKSPACE = 3,     /* ws NULL or smaller than required */
     CLEARMOE_ERR_HIP = 4,           /* a kernel launch failed */
     CLEARMOE_ERR_TOO_LARGE = 5      /* clearmoe_ffn_forward_noalloc: the shape
-                                       needs more than its fixed scratch */
+                                       needs more than its fixed scratch;
+                                       clearmoe_ffn_forward_few: too many tokens */
 } clearmoe_status;
 
 typedef enum { CLEARMOE_F32 = 0, CLEARMOE_BF16 = 1 } clearmoe_dtype;
@@ -109,8 +110,8 @@ const char* clearmoe_source_digest(void);
 const char* clearmoe_status_string(int status);
 
 /* Bytes of workspace clearmoe_ffn_forward needs for this shape (enough for
- * every entry point but clearmoe_ffn_forward_padded); 0 if the shape is
- * invalid. */
+ * every entry point but clearmoe_ffn_forward_padded and those with a
+ * workspace function of their own); 0 if the shape is invalid. */
 size_t clearmoe_workspace_bytes(const clearmoe_shape* shape);
 
 /* Router and top-k (Sec. III Phase 4 linear router, with the bias counted in
@@ -308,6 +309,118 @@ int clearmoe_ffn_forward_padded(const clearmoe_shape* shape, const void* x, cons
 int clearmoe_dense_ffn_forward(const clearmoe_shape* shape, const void* x, const void* W1,
                                const float* b1, const void* W2, const float* b2, void* y,
                                void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- The layer for a few tokens --------------------------------------------
+ * clearmoe_ffn_forward_ex for at most CLEARMOE_FEW_MAX_TOKENS tokens: the same
+ * arguments, layouts and results up to rounding (z, t and u keep float32's
+ * accuracy here, where the other entry points round them to dtype), as two
+ * kernels whose time hardly depends on the token count: the form for serving
+ * single tokens and small batches.
+ *   - Any router but one with class tokens (dense_stride > 0:
+ *     CLEARMOE_ERR_UNSUPPORTED).  Linear routers run inside the first kernel,
+ *     every logit in double; an MLP router runs before it, as
+ *     clearmoe_route_ex.
+ *   - Any D, H, r, q (r + k q <= 16384, else CLEARMOE_ERR_UNSUPPORTED); where
+ *     all are multiples of 8 (bf16) or 4 (float32) and every tensor is 16-byte
+ *     aligned, memory is read in 16-byte pieces, else element by element, for
+ *     which element alignment is enough (an MLP router's weights keep the
+ *     alignment clearmoe_route_ex asks for).
+ *   - More tokens: CLEARMOE_ERR_TOO_LARGE.
+ * The workspace holds clearmoe_few_workspace_bytes(shape) bytes, 256-byte
+ * aligned.  The kernels are timed as the stages CLEARMOE_STAGE_FC1 and
+ * CLEARMOE_STAGE_Y. */
+#define CLEARMOE_FEW_MAX_TOKENS 64
+
+/* 0 if the shape is invalid or the entry point does not take it. */
+size_t clearmoe_few_workspace_bytes(const clearmoe_shape* shape);
+
+int clearmoe_ffn_forward_few(const clearmoe_shape* shape, const clearmoe_router* router,
+                             const void* x, const void* W1, const float* b1, const void* US,
+                             const void* Vt, const float* b2, const void* P, const void* Q,
+                             void* y, int32_t* idx_out, float* gate_out, void* ws,
+                             size_t ws_bytes, hipStream_t stream);
+
+/* ---- 8-bit floating point with block scales ---------------------------------
+ * A quantised matrix [rows, cols] is two arrays:
+ *   values  rows of round_up(cols, 16) bytes, zeros past cols; a byte is an OCP
+ *           8-bit float, e4m3 (largest value 448, no infinity) or e5m2 (57344);
+ *   scales  for each block of 128 columns a byte b that stands for 2^(b - 127)
+ *           (255: NaN), in rows of round_up(ceil(cols / 128), 4) bytes.
+ * Activations have a row of scales for each row; weights, whose blocks are
+ * 128 x 128, one for each 128 rows.  The scales are powers of two so that
+ * dividing by them is exact and the matrix instructions apply them. */
+typedef enum { CLEARMOE_E4M3 = 2, CLEARMOE_E5M2 = 3 } clearmoe_byte_format;
+
+/* x [batch, rows, cols] (dtype CLEARMOE_F32 or CLEARMOE_BF16; rows ldx >= cols
+ * elements apart, batches rows * ldx) to values [batch, rows, .] and scales
+ * [batch, ceil(rows / block_rows), .] of a format; block_rows is 1
+ * (activations) or 128 (weights).  A block's scale is the smallest power of
+ * two, at least 2^-126, for which its largest finite magnitude stays within
+ * the format's range (1 for a block of zeros); every value is then rounded
+ * once, to nearest even.  NaN stays NaN, and so does infinity in e4m3; in e5m2
+ * infinity stays itself.  Bytes past cols are written as 0, scales past the
+ * last block as 1.  Pointers: x element-aligned (rows that start at 16-byte
+ * boundaries are read fastest), values 16-byte, scales 4-byte aligned.
+ * 1 <= cols <= 65536. */
+int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int64_t rows,
+                      int32_t cols, const void* x, int64_t ldx, void* values, void* scales,
+                      hipStream_t stream);
+
+/* A product C = epi(A B^T + bias) of quantised matrices, A [M, K] with row
+ * scales and B [N, K] with 128 x 128 scales, summed in float32 from the first
+ * to the last block.
+ *   M, N, K    M >= 0; N, K in 1 .. 65536, K a multiple of 16 (the width of the
+ *              value rows: zeros past the columns add nothing).
+ *   groups     0: one B.  E (1 .. 64): B [E, N, K], scales [E, ceil(N / 128), .]
+ *              and bias [E, N], one for each expert; rows offsets[e] ..
+ *              offsets[e + 1] of A and C (as clearmoe_dispatch leaves them, on
+ *              the device) belong to expert e.  Offsets are clamped to
+ *              [0, M]; rows of C outside all groups are left as they were.
+ *   a_format, b_format   CLEARMOE_E4M3 or CLEARMOE_E5M2, in any combination.
+ *   out        CLEARMOE_F32 or CLEARMOE_BF16: C [M, N], rounded once; or a byte
+ *              format: C is quantised as clearmoe_quantize with block_rows 1
+ *              would (from float32), values in C and scales in c_scale.
+ *   gelu       1: GELU after the bias.
+ *   lda, ldc   row strides in elements; 0: K, and N (byte formats:
+ *              round_up(N, 16)).  lda and a byte format's ldc are multiples
+ *              of 16; both at most 2^22.
+ * a, b and byte results are 16-byte aligned, scales 4-byte, F32 and BF16
+ * results element-aligned. */
+typedef struct {
+    int64_t M;
+    int32_t N, K;
+    int32_t groups;
+    int32_t a_format, b_format;
+    int32_t out;
+    int32_t gelu;
+    int32_t reserved;              /* must be 0 */
+    int64_t lda, ldc;
+} clearmoe_product;
+
+int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, const void* a_scale,
+                            const void* b, const void* b_scale, const float* bias,
+                            const int32_t* offsets, void* c, void* c_scale, hipStream_t stream);
+
+/* The dense FFN, or the caller's own experts' FFN between clearmoe_dispatch
+ * (with rows) and clearmoe_combine, in e4m3:
+ *     y = Q8(GELU(Q8(x) W1^T + b1)) W2^T + b2,
+ * Q8 quantising rows in blocks of 128 columns.  x, y [T, D] (dtype); W1 [H, D],
+ * W2 [D, H] quantised in e4m3 with 128 x 128 scales; biases float32 or NULL.
+ * With offsets [E + 1] (device), weights are [E, H, .] and [E, D, .], biases
+ * [E, H] and [E, D], and row p uses expert e with offsets[e] <= p <
+ * offsets[e + 1]; rows of y outside all groups are left as they were.
+ * With offsets NULL, E is ignored.  Uses T, D, H, E, dtype of the shape (any
+ * D and H; k, r, q must still be valid).  x and y need element alignment,
+ * weights 16-byte, their scales 4-byte.  The workspace holds
+ * clearmoe_quantized_workspace_bytes(shape) bytes, 256-byte aligned.  The
+ * products are timed as the stages CLEARMOE_STAGE_FC1 and
+ * CLEARMOE_STAGE_DENSE_FC2. */
+size_t clearmoe_quantized_workspace_bytes(const clearmoe_shape* shape);
+
+int clearmoe_quantized_ffn_forward(const clearmoe_shape* shape, const void* x, const void* W1,
+                                   const void* W1_scale, const float* b1, const void* W2,
+                                   const void* W2_scale, const float* b2, const int32_t* offsets,
+                                   void* y, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* ---- Stage timing (measurement support) -----------------------------------
  * Kernel stages of the entry points above.  While timing is on, the kernel of

@@ -20,7 +20,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libclearmoe.so")
 BUILD_DIR = os.path.join(ROOT, "_build", "clearmoe")
 SOURCES = ["api.cpp", "route.hip", "dispatch.hip", "gemm.hip", "gemm_bf16.hip", "fused.hip", "fused_split.hip",
-           "fused_cls.hip", "class_ffn.hip"]
+           "fused_cls.hip", "class_ffn.hip", "few.hip", "quantize.hip", "gemm_q8.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # The library carries the digest of the sources it was built from after this

@@ -21,7 +21,9 @@ __all__ = ["ClearMoEError", "Shape", "lib", "version", "workspace_bytes", "alloc
            "padded_workspace_bytes", "ffn_forward_padded", "ffn_forward_noalloc",
            "StackLayer", "make_stack_layer", "stack_shape", "stack_workspace_bytes",
            "stack_forward", "Router", "make_router", "route_ex",
-           "ffn_forward_ex"]
+           "ffn_forward_ex", "FEW_MAX_TOKENS", "few_workspace_bytes", "alloc_few_workspace",
+           "ffn_forward_few", "Product", "quantize", "quantized_gemm", "quantized_workspace_bytes",
+           "alloc_quantized_workspace", "quantized_ffn_forward"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libclearmoe.so")
@@ -33,9 +35,12 @@ SYMBOLS = ("clearmoe_version", "clearmoe_source_digest", "clearmoe_status_string
            "clearmoe_timing_start_sampled", "clearmoe_timing_stop", "clearmoe_padded_workspace_bytes",
            "clearmoe_ffn_forward_padded", "clearmoe_route_ex", "clearmoe_ffn_forward_ex",
            "clearmoe_ffn_forward_noalloc", "clearmoe_stack_workspace_bytes",
-           "clearmoe_stack_forward")
+           "clearmoe_stack_forward", "clearmoe_few_workspace_bytes", "clearmoe_ffn_forward_few",
+           "clearmoe_quantize", "clearmoe_quantized_gemm", "clearmoe_quantized_workspace_bytes",
+           "clearmoe_quantized_ffn_forward")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 ERR_TOO_LARGE = 5
+FEW_MAX_TOKENS = 64
 N_STAGES = 20
 
 
@@ -54,6 +59,14 @@ class Router(ctypes.Structure):
                 ("bh", ctypes.c_void_p), ("W2", ctypes.c_void_p), ("hidden", ctypes.c_int32),
                 ("adaptive", ctypes.c_int32), ("dense_stride", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("tau", ctypes.c_double)]
+
+
+class Product(ctypes.Structure):
+    """clearmoe_product: a product of quantised matrices."""
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("a_format", ctypes.c_int32), ("b_format", ctypes.c_int32), ("out", ctypes.c_int32),
+                ("gelu", ctypes.c_int32), ("reserved", ctypes.c_int32), ("lda", ctypes.c_int64),
+                ("ldc", ctypes.c_int64)]
 
 
 class StackLayer(ctypes.Structure):
@@ -120,6 +133,19 @@ def lib():
                                              vp]
         L.clearmoe_dense_ffn_forward.restype = ctypes.c_int
         L.clearmoe_dense_ffn_forward.argtypes = [sp] + [vp] * 6 + [vp, sz, vp]
+        L.clearmoe_few_workspace_bytes.restype = sz
+        L.clearmoe_few_workspace_bytes.argtypes = [sp]
+        L.clearmoe_ffn_forward_few.restype = ctypes.c_int
+        L.clearmoe_ffn_forward_few.argtypes = [sp, rp] + [vp] * 11 + [vp, sz, vp]
+        L.clearmoe_quantize.restype = ctypes.c_int
+        L.clearmoe_quantize.argtypes = [ctypes.c_int] * 3 + [ctypes.c_int64] * 2 + [ctypes.c_int32, vp,
+                                                                                  ctypes.c_int64, vp, vp, vp]
+        L.clearmoe_quantized_gemm.restype = ctypes.c_int
+        L.clearmoe_quantized_gemm.argtypes = [ctypes.POINTER(Product)] + [vp] * 9
+        L.clearmoe_quantized_workspace_bytes.restype = sz
+        L.clearmoe_quantized_workspace_bytes.argtypes = [sp]
+        L.clearmoe_quantized_ffn_forward.restype = ctypes.c_int
+        L.clearmoe_quantized_ffn_forward.argtypes = [sp] + [vp] * 10 + [sz, vp]
         L.clearmoe_stage_name.restype = ctypes.c_char_p
         L.clearmoe_stage_name.argtypes = [ctypes.c_int]
         L.clearmoe_timing_start.restype = ctypes.c_int
@@ -387,6 +413,165 @@ def stack_forward(x, layers, H: int, E: int, r: int, q: int, residual: bool = Tr
     rc = lib().clearmoe_stack_forward(ctypes.byref(s), arr, len(layers), 1 if residual else 0,
                                       _p(x), _p(y), _p(ws), ws.numel(), _stream(stream))
     _check(rc, "clearmoe_stack_forward")
+    return y
+
+
+def few_workspace_bytes(shape: Shape) -> int:
+    return int(lib().clearmoe_few_workspace_bytes(ctypes.byref(shape)))
+
+
+def _alloc(n: int, device) -> torch.Tensor:
+    if n == 0:
+        raise ClearMoEError("invalid shape")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_few_workspace(shape: Shape, device="cuda") -> torch.Tensor:
+    return _alloc(few_workspace_bytes(shape), device)
+
+
+def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
+                    ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    idx_out=None, gate_out=None, stream=None, renorm: int = 1):
+    """clearmoe_ffn_forward_few: the whole layer for at most FEW_MAX_TOKENS
+    tokens, with any router without class tokens.  Returns y."""
+    T, D = x.shape
+    E, _, q = P.shape
+    s = make_shape(T, D, E, k, _dt(x), H=W1.shape[0], r=US.shape[1], q=q, renorm=renorm)
+    ws = alloc_few_workspace(s, x.device) if ws is None else ws
+    y = torch.empty((T, D), dtype=x.dtype, device=x.device) if out is None else out
+    rc = lib().clearmoe_ffn_forward_few(ctypes.byref(s), ctypes.byref(router), _p(x), _p(W1),
+                                        _p(b1), _p(US), _p(Vt), _p(b2), _p(P), _p(Q), _p(y),
+                                        _p(idx_out), _p(gate_out), _p(ws), ws.numel(),
+                                        _stream(stream))
+    _check(rc, "clearmoe_ffn_forward_few")
+    return y
+
+
+# 8-bit formats, and the C ABI's numbers of every output type
+_FORMATS = {torch.float8_e4m3fn: 2, torch.float8_e5m2: 3}
+_OUTS = {torch.float32: F32, torch.bfloat16: BF16, **_FORMATS}
+
+
+def _format(dtype) -> int:
+    if dtype not in _FORMATS:
+        raise ClearMoEError(f"unsupported 8-bit format {dtype}")
+    return _FORMATS[dtype]
+
+
+def _value_cols(cols: int) -> int:
+    return (cols + 15) // 16 * 16
+
+
+def _scale_cols(cols: int) -> int:
+    return (cols + 511) // 512 * 4
+
+
+def _scales(s: torch.Tensor, shape, what: str) -> ctypes.c_void_p:
+    if s.dtype != torch.float8_e8m0fnu or tuple(s.shape) != tuple(shape):
+        raise ClearMoEError(f"{what} must be float8_e8m0fnu {tuple(shape)}, not {s.dtype} {tuple(s.shape)}")
+    return _p(s)
+
+
+def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
+    """clearmoe_quantize: x [rows, cols] or [batch, rows, cols] (rows may be
+    strided) in 8-bit floating point with a power-of-two scale for each block
+    of block_rows (1 or 128) x 128 values.  Returns (values [..., rows, cols up
+    to a multiple of 16] in fmt, scales [..., ceil(rows / block_rows), column
+    blocks up to a multiple of 4] in float8_e8m0fnu)."""
+    if x.dim() not in (2, 3):
+        raise ClearMoEError("quantize takes [rows, cols] or [batch, rows, cols]")
+    batch = x.shape[0] if x.dim() == 3 else 1
+    rows, cols = x.shape[-2:]
+    ldx = x.stride(-2) if rows > 1 else max(cols, 1)
+    if batch > 1 and rows == 1:
+        ldx = x.stride(0)
+    if not x.is_cuda:
+        raise ClearMoEError("tensor is not on the GPU")
+    if x.numel() > 0 and ((cols > 1 and x.stride(-1) != 1) or (batch > 1 and x.stride(0) != rows * ldx)):
+        raise ClearMoEError("rows must be contiguous and evenly spaced over the batch")
+    lead = tuple(x.shape[:-2])
+    v = torch.empty(lead + (rows, _value_cols(cols)), dtype=fmt, device=x.device)
+    nr = rows if block_rows == 1 else -(-rows // 128)
+    s = torch.empty(lead + (nr, _scale_cols(cols)), dtype=torch.float8_e8m0fnu, device=x.device)
+    rc = lib().clearmoe_quantize(_dt(x), _format(fmt), block_rows, batch, rows, cols,
+                                 ctypes.c_void_p(x.data_ptr()), ldx, _p(v), _p(s), _stream(stream))
+    _check(rc, "clearmoe_quantize")
+    return v, s
+
+
+def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offsets=None,
+                   out_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None):
+    """clearmoe_quantized_gemm: a [M, K] with 1 x 128 scales times b [N, K] with
+    128 x 128 scales, as quantize returns them, or, with offsets [E + 1], times
+    b [E, N, K] for the rows of each expert (rows outside all groups are left
+    as out had them).  Returns C [M, N] in out_dtype; for an 8-bit out_dtype
+    (values [M, N up to a multiple of 16], scales)."""
+    M, K = a.shape
+    grouped = offsets is not None
+    E = b.shape[0] if grouped else 0
+    N = b.shape[-2]
+    if b.dim() != (3 if grouped else 2) or b.shape[-1] != K:
+        raise ClearMoEError(f"b must be [{'E, ' if grouped else ''}N, {K}], not {tuple(b.shape)}")
+    lead = (E,) if grouped else ()
+    if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != lead + (N,)):
+        raise ClearMoEError(f"bias must be float32 {lead + (N,)}")
+    if grouped and (offsets.dtype != torch.int32 or tuple(offsets.shape) != (E + 1,)):
+        raise ClearMoEError(f"offsets must be int32 {(E + 1,)}")
+    if out_dtype not in _OUTS:
+        raise ClearMoEError(f"unsupported dtype {out_dtype}")
+    byte = out_dtype in _FORMATS
+    cols = _value_cols(N) if byte else N
+    c = torch.empty((M, cols), dtype=out_dtype, device=a.device) if out is None else out
+    if c.dtype != out_dtype or tuple(c.shape) != (M, cols):
+        raise ClearMoEError(f"out must be {out_dtype} {(M, cols)}")
+    cs = torch.empty((M, _scale_cols(N)), dtype=torch.float8_e8m0fnu, device=a.device) if byte else None
+    p = Product(M, N, K, E, _format(a.dtype), _format(b.dtype), _OUTS[out_dtype], int(gelu), 0, 0, 0)
+    rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), _p(a), _scales(a_scale, (M, _scale_cols(K)), "a_scale"),
+                                       _p(b), _scales(b_scale, lead + (-(-N // 128), _scale_cols(K)), "b_scale"),
+                                       _p(bias), _p(offsets), _p(c), _p(cs), _stream(stream))
+    _check(rc, "clearmoe_quantized_gemm")
+    return (c, cs) if byte else c
+
+
+def quantized_workspace_bytes(shape: Shape) -> int:
+    return int(lib().clearmoe_quantized_workspace_bytes(ctypes.byref(shape)))
+
+
+def alloc_quantized_workspace(shape: Shape, device="cuda") -> torch.Tensor:
+    return _alloc(quantized_workspace_bytes(shape), device)
+
+
+def quantized_ffn_forward(x, W1, W1_scale, b1, W2, W2_scale, b2, offsets=None,
+                          ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                          stream=None):
+    """clearmoe_quantized_ffn_forward: x [T, D] through an FFN with e4m3 weights
+    (quantize(W, block_rows=128): W1 [H, .], W2 [D, .]), or, with offsets
+    [E + 1], rows sorted by expert through their expert's ([E, H, .],
+    [E, D, .]; rows outside all groups are left as out had them)."""
+    T, D = x.shape
+    grouped = offsets is not None
+    lead = (W1.shape[0],) if grouped else ()
+    E, H = (lead[0] if grouped else 1), W1.shape[-2]
+    for w, n, kk in ((W1, H, D), (W2, D, H)):
+        if w.dtype != torch.float8_e4m3fn or tuple(w.shape) != lead + (n, _value_cols(kk)):
+            raise ClearMoEError(f"weights must be float8_e4m3fn {lead + (n, _value_cols(kk))}, not "
+                                f"{w.dtype} {tuple(w.shape)}")
+    for b, n in ((b1, H), (b2, D)):
+        if b is not None and (b.dtype != torch.float32 or tuple(b.shape) != lead + (n,)):
+            raise ClearMoEError(f"biases must be float32 {lead + (n,)}")
+    if grouped and (offsets.dtype != torch.int32 or tuple(offsets.shape) != (E + 1,)):
+        raise ClearMoEError(f"offsets must be int32 {(E + 1,)}")
+    s = make_shape(T, D, E, 1, _dt(x), H=H)
+    ws = alloc_quantized_workspace(s, x.device) if ws is None else ws
+    y = torch.empty((T, D), dtype=x.dtype, device=x.device) if out is None else out
+    if y.dtype != x.dtype or y.shape != x.shape:
+        raise ClearMoEError("out must have x's shape and dtype")
+    rc = lib().clearmoe_quantized_ffn_forward(
+        ctypes.byref(s), _p(x), _p(W1), _scales(W1_scale, lead + (-(-H // 128), _scale_cols(D)), "W1_scale"), _p(b1),
+        _p(W2), _scales(W2_scale, lead + (-(-D // 128), _scale_cols(H)), "W2_scale"), _p(b2), _p(offsets), _p(y),
+        _p(ws), ws.numel(), _stream(stream))
+    _check(rc, "clearmoe_quantized_ffn_forward")
     return y
 
 

@@ -9,7 +9,9 @@
 #include <vector>
 
 #include "class_ffn.h"
+#include "few.h"
 #include "kernels.h"
+#include "q8.h"
 
 using namespace clearmoe;
 
@@ -1498,6 +1500,231 @@ int clearmoe_stack_forward(const clearmoe_shape* shape, const clearmoe_stack_lay
     }
     return CLEARMOE_OK;
 }
+
+}  // extern "C"
+
+namespace {
+
+// Workspace of the few-token layer: the routing and the partial sums, and for
+// an MLP router the workspace of clearmoe_route_ex.
+struct FewLayout {
+    size_t idx, gate, part, route, total;
+};
+constexpr int64_t kFewMaxColumns = 16384;      // r + k q: the second kernel's LDS
+int check_few(const clearmoe_shape* shape) {
+    const int rc = check_shape(shape, true, true);
+    if (rc != CLEARMOE_OK) return rc;
+    if (shape->T > CLEARMOE_FEW_MAX_TOKENS) return CLEARMOE_ERR_TOO_LARGE;
+    if (shape->r + static_cast<int64_t>(shape->k) * shape->q > kFewMaxColumns) return CLEARMOE_ERR_UNSUPPORTED;
+    return CLEARMOE_OK;
+}
+FewLayout few_layout(const clearmoe_shape& s) {
+    FewLayout L{};
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off += up(bytes > 0 ? bytes : 1);
+        return at;
+    };
+    L.idx = take(sizeof(int32_t) * s.T * s.k);
+    L.gate = take(sizeof(float) * s.T * s.k);
+    L.part = take(few_part_bytes(s.dtype, s.T, s.H, s.r, s.k, s.q));
+    L.route = off;
+    clearmoe_shape rs = s;
+    rs.H = rs.r = rs.q = 0;
+    off += up(clearmoe_workspace_bytes(&rs));
+    L.total = off;
+    return L;
+}
+
+struct QuantizedLayout {
+    size_t xv, xs, zv, zs, total;
+};
+QuantizedLayout quantized_layout(const clearmoe_shape& s) {
+    QuantizedLayout L{};
+    size_t off = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t at = off;
+        off += up(static_cast<size_t>(s.T) * static_cast<size_t>(bytes) + 1);
+        return at;
+    };
+    L.xv = take(q8_cols(s.D));
+    L.xs = take(q8_scale_cols(s.D));
+    L.zv = take(q8_cols(s.H));
+    L.zs = take(q8_scale_cols(s.H));
+    L.total = off;
+    return L;
+}
+bool byte_format(int f) { return f == CLEARMOE_E4M3 || f == CLEARMOE_E5M2; }
+constexpr int64_t kMaxStride = int64_t{1} << 22;
+
+}  // namespace
+
+extern "C" {
+
+size_t clearmoe_few_workspace_bytes(const clearmoe_shape* shape) {
+    return check_few(shape) == CLEARMOE_OK ? few_layout(*shape).total : 0;
+}
+
+int clearmoe_ffn_forward_few(const clearmoe_shape* shape, const clearmoe_router* router,
+                             const void* x, const void* W1, const float* b1, const void* US,
+                             const void* Vt, const float* b2, const void* P, const void* Q,
+                             void* y, int32_t* idx_out, float* gate_out, void* ws,
+                             size_t ws_bytes, hipStream_t stream) {
+    int rc = check_few(shape);
+    if (rc != CLEARMOE_OK) return rc;
+    const clearmoe_shape& s = *shape;
+    const size_t es = elem_size(s.dtype);
+    if (!W1 || (s.T > 0 && (!x || !y))) return CLEARMOE_ERR_INVALID_ARG;
+    if (s.r > 0 && (!US || !Vt)) return CLEARMOE_ERR_INVALID_ARG;
+    if (s.q > 0 && (!P || !Q)) return CLEARMOE_ERR_INVALID_ARG;
+    const void* ve[] = {x, W1, US, Vt, P, Q, y};
+    for (const void* p : ve)
+        if (p && !aligned(p, es)) return CLEARMOE_ERR_INVALID_ARG;
+    const void* v4[] = {b1, b2, idx_out, gate_out};
+    for (const void* p : v4)
+        if (p && !aligned(p, 4)) return CLEARMOE_ERR_INVALID_ARG;
+    const bool mlp = router != nullptr && router->hidden > 0;
+    rc = check_router(s, router, mlp && !unaligned_rows(s) ? 16 : es);
+    if (rc != CLEARMOE_OK) return rc;
+    if (router->dense_stride > 0) return CLEARMOE_ERR_UNSUPPORTED;
+    const FewLayout L = few_layout(s);
+    if (!ws || !aligned(ws, kAlign) || ws_bytes < L.total) return CLEARMOE_ERR_WORKSPACE;
+    if (s.T == 0) return CLEARMOE_OK;
+
+    FewArgs a{};
+    a.x = x; a.W1 = W1; a.US = US; a.Vt = Vt; a.P = P; a.Q = Q; a.Wg = router->Wg;
+    a.b1 = b1; a.b2 = b2; a.bg = router->bg;
+    a.y = y;
+    a.idx = idx_out ? idx_out : at<int32_t>(ws, L.idx);
+    a.gate = gate_out ? gate_out : at<float>(ws, L.gate);
+    a.part = at<float>(ws, L.part);
+    a.T = s.T; a.D = s.D; a.H = s.H; a.E = s.E; a.k = s.k; a.r = s.r; a.q = s.q;
+    a.adaptive = router->adaptive; a.renorm = s.renorm; a.tau = router->tau;
+    a.routed = mlp ? 1 : 0;
+    if (mlp) {
+        clearmoe_shape rs = s;              // the routing alone, as few_layout counts it
+        rs.H = rs.r = rs.q = 0;
+        rc = clearmoe_route_ex(&rs, router, x, a.idx, a.gate, at<void>(ws, L.route), ws_bytes - L.route, stream);
+        if (rc != CLEARMOE_OK) return rc;
+    }
+    bool whole = !unaligned_layer(s);
+    for (const void* p : {x, W1, US, Vt, P, Q, router->Wg})
+        whole = whole && (p == nullptr || aligned(p, 16));
+    CLEARMOE_STAGE(CLEARMOE_STAGE_FC1, stream, launch_few_hidden(s.dtype, whole, a, stream));
+    CLEARMOE_STAGE(CLEARMOE_STAGE_Y, stream, launch_few_out(s.dtype, whole, a, stream));
+    return CLEARMOE_OK;
+}
+
+int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int64_t rows,
+                      int32_t cols, const void* x, int64_t ldx, void* values, void* scales,
+                      hipStream_t stream) {
+    if (dtype != CLEARMOE_F32 && dtype != CLEARMOE_BF16) return CLEARMOE_ERR_UNSUPPORTED;
+    if (!byte_format(format)) return CLEARMOE_ERR_UNSUPPORTED;
+    if (block_rows != 1 && block_rows != kQ8Block) return CLEARMOE_ERR_INVALID_ARG;
+    if (cols < 1 || cols > kMaxDim || batch < 0 || rows < 0 || ldx < cols) return CLEARMOE_ERR_INVALID_ARG;
+    if (batch == 0 || rows == 0) return CLEARMOE_OK;
+    // one workgroup for 16 row blocks or for a 128 x 128 block: the grid's
+    // limit, checked so that no product overflows
+    constexpr int64_t kMostBlocks = int64_t{1} << 31;
+    if (rows >= kMostBlocks || batch >= kMostBlocks || ldx > (int64_t{1} << 40)) return CLEARMOE_ERR_INVALID_ARG;
+    const int64_t per = block_rows == 1 ? rows : (rows + kQ8Block - 1) / kQ8Block;
+    if (batch > kMostBlocks / per || batch * per > kMostBlocks / q8_blocks(cols)) return CLEARMOE_ERR_INVALID_ARG;
+    if (!x || !values || !scales) return CLEARMOE_ERR_INVALID_ARG;
+    if (!aligned(x, elem_size(dtype)) || !aligned(values, 16) || !aligned(scales, 4)) return CLEARMOE_ERR_INVALID_ARG;
+    if (launch_quantize(dtype, format - CLEARMOE_E4M3, block_rows, batch, rows, cols, x, ldx,
+                        static_cast<uint8_t*>(values), static_cast<uint8_t*>(scales), stream) != hipSuccess)
+        return CLEARMOE_ERR_HIP;
+    return CLEARMOE_OK;
+}
+
+int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, const void* a_scale,
+                            const void* b, const void* b_scale, const float* bias,
+                            const int32_t* offsets, void* c, void* c_scale, hipStream_t stream) {
+    if (product == nullptr) return CLEARMOE_ERR_INVALID_ARG;
+    const clearmoe_product& p = *product;
+    const bool bytes = byte_format(p.out);
+    if (!byte_format(p.a_format) || !byte_format(p.b_format)) return CLEARMOE_ERR_UNSUPPORTED;
+    if (!bytes && p.out != CLEARMOE_F32 && p.out != CLEARMOE_BF16) return CLEARMOE_ERR_UNSUPPORTED;
+    if (p.M < 0 || p.M >= (int64_t{1} << 31) || p.N < 1 || p.N > kMaxDim || p.K < 16 || p.K > kMaxDim ||
+        p.K % 16 != 0)
+        return CLEARMOE_ERR_INVALID_ARG;
+    if (p.groups < 0 || p.groups > 64 || (p.gelu != 0 && p.gelu != 1) || p.reserved != 0)
+        return CLEARMOE_ERR_INVALID_ARG;
+    const int64_t cols = bytes ? q8_cols(p.N) : p.N;
+    const int64_t lda = p.lda != 0 ? p.lda : p.K, ldc = p.ldc != 0 ? p.ldc : cols;
+    if (lda < p.K || lda > kMaxStride || lda % 16 != 0) return CLEARMOE_ERR_INVALID_ARG;
+    if (ldc < cols || ldc > kMaxStride || (bytes && ldc % 16 != 0)) return CLEARMOE_ERR_INVALID_ARG;
+    if (!b || !b_scale || (p.M > 0 && (!a || !a_scale || !c || (bytes && !c_scale)))) return CLEARMOE_ERR_INVALID_ARG;
+    if ((p.groups > 0) != (offsets != nullptr)) return CLEARMOE_ERR_INVALID_ARG;
+    if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) || !aligned(c_scale, 4) ||
+        !aligned(bias, 4) || !aligned(offsets, 4) || !aligned(c, bytes ? 16 : elem_size(p.out)))
+        return CLEARMOE_ERR_INVALID_ARG;
+    if (p.M == 0) return CLEARMOE_OK;
+    Q8Desc g{};
+    g.A = static_cast<const uint8_t*>(a); g.lda = lda;
+    g.SA = static_cast<const uint8_t*>(a_scale); g.sa_ld = q8_scale_cols(p.K);
+    g.B = static_cast<const uint8_t*>(b); g.b_seg_stride = static_cast<int64_t>(p.N) * p.K;
+    g.SB = static_cast<const uint8_t*>(b_scale); g.sb_ld = q8_scale_cols(p.K);
+    g.sb_seg_stride = q8_blocks(p.N) * g.sb_ld;
+    g.bias = bias;
+    g.C = c; g.ldc = ldc;
+    g.SC = static_cast<uint8_t*>(c_scale); g.sc_ld = q8_scale_cols(p.N);
+    g.out = p.out == CLEARMOE_F32 ? kQ8OutF32 : p.out == CLEARMOE_BF16 ? kQ8OutBf16
+            : p.out == CLEARMOE_E4M3 ? kQ8OutE4M3 : kQ8OutE5M2;
+    g.gelu = p.gelu;
+    g.fa = p.a_format - CLEARMOE_E4M3; g.fb = p.b_format - CLEARMOE_E4M3;
+    g.wide = aligned(c, 16) && ldc % piece_elems(p.out) == 0 && p.N % piece_elems(p.out) == 0;
+    g.M = p.M; g.N = p.N; g.K = p.K;
+    g.seg_offsets = offsets; g.nseg = p.groups;
+    return launch_gemm_q8(g, stream) == hipSuccess ? CLEARMOE_OK : CLEARMOE_ERR_HIP;
+}
+
+size_t clearmoe_quantized_workspace_bytes(const clearmoe_shape* shape) {
+    return check_shape(shape, true, true) == CLEARMOE_OK ? quantized_layout(*shape).total : 0;
+}
+
+int clearmoe_quantized_ffn_forward(const clearmoe_shape* shape, const void* x, const void* W1,
+                                   const void* W1_scale, const float* b1, const void* W2,
+                                   const void* W2_scale, const float* b2, const int32_t* offsets,
+                                   void* y, void* ws, size_t ws_bytes, hipStream_t stream) {
+    int rc = check_shape(shape, true, true);
+    if (rc != CLEARMOE_OK) return rc;
+    const clearmoe_shape& s = *shape;
+    const size_t es = elem_size(s.dtype);
+    if (!W1 || !W1_scale || !W2 || !W2_scale || (s.T > 0 && (!x || !y))) return CLEARMOE_ERR_INVALID_ARG;
+    if (!aligned(W1, 16) || !aligned(W2, 16) || !aligned(x, es) || !aligned(y, es)) return CLEARMOE_ERR_INVALID_ARG;
+    const void* v4[] = {W1_scale, W2_scale, b1, b2, offsets};
+    for (const void* p : v4)
+        if (p && !aligned(p, 4)) return CLEARMOE_ERR_INVALID_ARG;
+    const QuantizedLayout L = quantized_layout(s);
+    if (!ws || !aligned(ws, kAlign) || ws_bytes < L.total) return CLEARMOE_ERR_WORKSPACE;
+    if (s.T == 0) return CLEARMOE_OK;
+    rc = clearmoe_quantize(s.dtype, CLEARMOE_E4M3, 1, 1, s.T, s.D, x, s.D, at<void>(ws, L.xv), at<void>(ws, L.xs),
+                           stream);
+    if (rc != CLEARMOE_OK) return rc;
+    clearmoe_product p{};
+    p.M = s.T; p.N = s.H; p.K = static_cast<int32_t>(q8_cols(s.D));
+    p.groups = offsets ? s.E : 0;
+    p.a_format = p.b_format = p.out = CLEARMOE_E4M3;
+    p.gelu = 1;
+    {
+        StageScope scope(CLEARMOE_STAGE_FC1, stream);
+        rc = clearmoe_quantized_gemm(&p, at<void>(ws, L.xv), at<void>(ws, L.xs), W1, W1_scale, b1, offsets,
+                                     at<void>(ws, L.zv), at<void>(ws, L.zs), stream);
+    }
+    if (rc != CLEARMOE_OK) return rc;
+    p.N = s.D; p.K = static_cast<int32_t>(q8_cols(s.H));
+    p.out = s.dtype;
+    p.gelu = 0;
+    StageScope scope(CLEARMOE_STAGE_DENSE_FC2, stream);
+    return clearmoe_quantized_gemm(&p, at<void>(ws, L.zv), at<void>(ws, L.zs), W2, W2_scale, b2, offsets, y,
+                                   nullptr, stream);
+}
+
+}  // extern "C"
+
+extern "C" {
 
 const char* clearmoe_stage_name(int stage) {
     static const char* names[CLEARMOE_N_STAGES] = {

@@ -1,0 +1,88 @@
+// 8-bit floating point with block scales: internal declarations of the
+// quantiser (quantize.hip) and the products (gemm_q8.hip).
+//
+// A matrix of k columns is held as rows of round_up(k, 16) bytes (zeros past
+// k) and, for each block of 128 columns of a row (or of 128 rows), one byte b
+// that stands for the scale 2^(b - 127); rows of scales have
+// q8_scale_cols(k) bytes, whole 4-byte words.
+#pragma once
+
+#include "kernels.h"
+
+namespace clearmoe {
+
+constexpr int kQ8Block = 128;
+constexpr int kQ8One = 127;              // the scale byte of 1
+
+__host__ __device__ inline int64_t q8_cols(int64_t k) { return (k + 15) / 16 * 16; }
+__host__ __device__ inline int64_t q8_blocks(int64_t k) { return (k + kQ8Block - 1) / kQ8Block; }
+__host__ __device__ inline int64_t q8_scale_cols(int64_t k) { return (q8_blocks(k) + 3) / 4 * 4; }
+
+// Formats, as the matrix instructions number them, and output types.
+enum { kQ8E4M3 = 0, kQ8E5M2 = 1 };
+enum { kQ8OutF32 = 0, kQ8OutBf16 = 1, kQ8OutE4M3 = 2, kQ8OutE5M2 = 3 };
+
+// Largest finite value 1.75 * 2^kTopExp of a format.
+__host__ __device__ constexpr int q8_top_exp(int fmt) { return fmt == kQ8E4M3 ? 8 : 15; }
+
+// The scale exponent of a block whose largest finite magnitude has the bits u:
+// the smallest e with amax <= 1.75 2^(top + e), at least -126; 0 for zeros.
+// (Adding 0x1fffff carries into the exponent exactly when the mantissa is
+// above 1.75.)
+__device__ __forceinline__ int q8_exponent(uint32_t u, int top) {
+    if (u == 0) return 0;
+    const int e = static_cast<int>((u + 0x1fffffu) >> 23) - 127 - top;
+    return e < -126 ? -126 : e;
+}
+__device__ __forceinline__ float q8_two_to(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+// |v| for the block's maximum: infinities and NaN do not set a scale.
+__device__ __forceinline__ float q8_mag(float v) {
+    const float m = fabsf(v);
+    return m < __builtin_inff() ? m : 0.0f;
+}
+// Four floats -> four bytes, round to nearest even; infinities become NaN in
+// e4m3 (which has none) and stay in e5m2.
+template <int FMT>
+__device__ __forceinline__ uint32_t q8_pack4(float a, float b, float c, float d) {
+    int v = 0;
+    if constexpr (FMT == kQ8E4M3) {
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, v, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+    } else {
+        v = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, v, false);
+        v = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, v, true);
+    }
+    return static_cast<uint32_t>(v);
+}
+
+// x [batch, rows, cols] (dtype, row stride ldx elements, batches rows * ldx
+// apart) -> v, scale; block_rows 1 or 128.
+hipError_t launch_quantize(int dtype, int fmt, int block_rows, int64_t batch, int64_t rows, int64_t cols,
+                           const void* x, int64_t ldx, uint8_t* v, uint8_t* scale, hipStream_t st);
+
+// C[m, n] = epi( sum over blocks of 2^(sa + sb) sum_k A[m, k] B_seg(m)[n, k] ).
+struct Q8Desc {
+    const uint8_t* A;            // [M, >= K] row stride lda bytes
+    int64_t lda;
+    const uint8_t* SA;           // [M, sa_ld]
+    int64_t sa_ld;
+    const uint8_t* B;            // [N, K] per segment
+    int64_t b_seg_stride;
+    const uint8_t* SB;           // [ceil(N / 128), q8_scale_cols(K)] per segment
+    int64_t sb_ld, sb_seg_stride;
+    const float* bias;           // [N] per segment, or null
+    void* C;                     // row stride ldc elements
+    int64_t ldc;
+    uint8_t* SC;                 // 8-bit output: its scales, row stride sc_ld
+    int64_t sc_ld;
+    int out, gelu, fa, fb;
+    int wide;                    // C rows can be stored 16 bytes at a time
+    int64_t M;
+    int N, K;                    // K a multiple of 16
+    const int32_t* seg_offsets;  // [nseg + 1] on the device, or null
+    int nseg;
+    int seg_merge;               // always 0 (the tile search's field)
+};
+hipError_t launch_gemm_q8(const Q8Desc& g, hipStream_t st);
+
+}  // namespace clearmoe

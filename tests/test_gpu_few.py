@@ -1,0 +1,281 @@
+"""The whole layer for a few tokens (ffn_forward_few) against a plain 64-bit
+form: types, widths, token counts, routers and gates, and where it runs (a
+stream of its own, captured graphs, a shared workspace)."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_28516_amd import clearmoe as cm
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _layer(T, D, H, E, k, r, q, dtype, seed, mlp=0):
+    g = torch.Generator().manual_seed(seed)
+    n = lambda *s: torch.randn(*s, generator=g)
+    L = dict(x=n(T, D), W1=n(H, D) / math.sqrt(D), US=n(D, r) / math.sqrt(max(r, 1)), Vt=n(r, H) / math.sqrt(H),
+             P=n(E, D, q) / math.sqrt(max(q, 1)), Q=n(E, q, H) / math.sqrt(H), Wg=n(E, mlp or D) / math.sqrt(D))
+    if mlp:
+        L["Wh"] = n(mlp, D) / math.sqrt(D)
+    L = {a: t.to(dtype).cuda() for a, t in L.items()}
+    L.update(b1=(0.1 * n(H)).cuda(), b2=(0.1 * n(D)).cuda(), bg=(0.1 * n(E)).cuda())
+    if mlp:
+        L["bh"] = (0.1 * n(mlp)).cuda()
+    L["k"] = k
+    return L
+
+
+def _router(L, **kw):
+    return cm.make_router(L["Wg"], L["bg"], L.get("Wh"), L.get("bh"), **kw)
+
+
+def _few(L, router, renorm=1, **kw):
+    T, k = L["x"].shape[0], L["k"]
+    idx = torch.full((T, k), -7, dtype=torch.int32, device="cuda")
+    gate = torch.full((T, k), -7.0, dtype=F32, device="cuda")
+    y = cm.ffn_forward_few(L["x"], L["W1"], L["b1"], L["US"], L["Vt"], L["b2"], L["P"], L["Q"], router, k,
+                           idx_out=idx, gate_out=gate, renorm=renorm, **kw)
+    return y, idx, gate
+
+
+def _gelu(v):
+    return 0.5 * v * torch.special.erfc(-v / math.sqrt(2.0))
+
+
+def _route(L, renorm, adaptive=False, tau=0.0):
+    x, k = L["x"].double().cpu(), L["k"]
+    if "Wh" in L:
+        x = _gelu(x @ L["Wh"].double().cpu().T + L["bh"].double().cpu()).to(L["x"].dtype).double()
+    lg = x @ L["Wg"].double().cpu().T + L["bg"].double().cpu()
+    v, i = torch.sort(lg, dim=1, descending=True, stable=True)
+    p = torch.softmax(lg, dim=1).gather(1, i[:, :k])
+    gate = p / p.sum(1, keepdim=True) if renorm else p
+    idx = i[:, :k].clone()
+    if adaptive:
+        sure = p[:, 0] >= tau
+        idx[sure, 1] = -1
+        gate[sure, 1] = 0.0
+        if renorm:
+            gate[sure, 0] = 1.0
+    # smallest gap that decides the choice
+    m = min(k + 1, v.shape[1])
+    gap = (v[:, :m - 1] - v[:, 1:m]).amin(1) if m > 1 else torch.full((v.shape[0],), math.inf)
+    if adaptive:
+        gap = torch.minimum(gap, (p[:, 0] - tau).abs())
+    return idx, gate, gap
+
+
+def _reference(L, idx, gate):
+    """y in 64 bits for a given routing, and a bound on the float32 arithmetic:
+    n products summed in any order are off by at most (n + 2) 2^-24 of the sum
+    of their magnitudes, the GELU by 1.5e-7 / 2 of its argument and a few
+    roundings, with a slope of at most 1.13; in bfloat16, z as two parts is
+    off by 2^-16 of itself."""
+    f = {a: L[a].double().cpu() for a in ("x", "W1", "b1", "US", "Vt", "b2", "P", "Q")}
+    u = 2.0 ** -24
+    D, H, r, q = f["x"].shape[1], f["W1"].shape[0], f["US"].shape[1], f["Q"].shape[1]
+    pre = f["x"] @ f["W1"].T + f["b1"]
+    z = _gelu(pre)
+    dz = 1.13 * (D + 4) * u * (f["x"].abs() @ f["W1"].abs().T + f["b1"].abs()) + 4e-7 * pre.abs()
+    if L["x"].dtype == BF16:
+        dz = dz + 2.0 ** -16 * z.abs()
+    za = z.abs() + dz
+    su = (H + 4) * u
+    y = (z @ f["Vt"].T) @ f["US"].T + f["b2"]
+    mass = (za @ f["Vt"].abs().T) @ f["US"].abs().T + f["b2"].abs()
+    dy = ((dz + su * za) @ f["Vt"].abs().T) @ f["US"].abs().T
+    for t in range(y.shape[0]):
+        for j in range(idx.shape[1]):
+            e = int(idx[t, j])
+            if e < 0:
+                continue
+            y[t] += gate[t, j] * (f["P"][e] @ (f["Q"][e] @ z[t]))
+            m = abs(gate[t, j]) * (f["P"][e].abs() @ (f["Q"][e].abs() @ za[t]))
+            mass[t] += m
+            dy[t] += abs(gate[t, j]) * (f["P"][e].abs() @ (f["Q"][e].abs() @ (dz[t] + su * za[t]))) + 2.0 ** -23 * m
+    return y, dy + (r + idx.shape[1] * q + 6) * u * mass
+
+
+def _check(L, router, renorm=1, adaptive=False, tau=0.0, **kw):
+    y, idx, gate = _few(L, router, renorm, **kw)
+    ri, rg, gap = _route(L, renorm, adaptive, tau)
+    sure = gap > 1e-9
+    assert sure.all() or "Wh" in L
+    assert torch.equal(idx.cpu().long()[sure], ri[sure])
+    assert ((gate.cpu().double() - rg)[sure].abs() <= 2.0 ** -22).all()
+    ref, d = _reference(L, idx.cpu(), gate.cpu().double())
+    half = torch.finfo(y.dtype).eps / 2
+    err = (y.cpu().double() - ref).abs()
+    bad = err > half * ref.abs() + (1 + half) * d
+    assert not bad.any(), (int(bad.sum()), bad.nonzero()[:4].tolist(), float(err.max()))
+    # float32's share is far below the rounding of a bfloat16 result
+    if y.dtype == BF16 and ref.numel() > 500:
+        assert err.norm() <= 2.0 ** -8 * ref.norm()
+    return y, idx, gate
+
+
+SHAPES = [
+    # T, D, H, E, k, r, q
+    (1, 8, 8, 1, 1, 0, 0), (1, 8, 16, 2, 2, 8, 8), (1, 384, 1536, 8, 1, 128, 32), (1, 768, 3072, 8, 2, 256, 64),
+    (2, 192, 768, 4, 1, 64, 16), (5, 390, 1550, 6, 2, 100, 27), (3, 1, 1, 1, 1, 1, 1), (7, 33, 65, 3, 3, 17, 5),
+    (15, 200, 808, 16, 4, 40, 24), (16, 768, 3072, 8, 2, 256, 64), (17, 136, 520, 8, 2, 48, 16),
+    (33, 100, 401, 5, 2, 30, 7), (64, 384, 1536, 8, 2, 128, 32), (9, 64, 96, 64, 64, 8, 8), (4, 128, 256, 4, 2, 32, 0),
+    (4, 128, 256, 4, 2, 0, 16), (2, 2048, 264, 8, 2, 64, 32), (1, 24, 5000, 2, 1, 24, 24),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("T,D,H,E,k,r,q", SHAPES)
+def test_linear_router(T, D, H, E, k, r, q, renorm, dtype):
+    L = _layer(T, D, H, E, k, r, q, dtype, T * 13 + D + H)
+    _check(L, _router(L), renorm)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("tau", [0.0, 0.5, 0.9, 2.0])
+@pytest.mark.parametrize("T,D,H,E,r,q", [(1, 384, 1536, 8, 128, 32), (16, 200, 520, 5, 48, 16), (21, 70, 300, 4, 20, 9)])
+def test_adaptive_router(T, D, H, E, r, q, tau, renorm, dtype):
+    L = _layer(T, D, H, E, 2, r, q, dtype, T + D)
+    L["Wg"] = (3 * L["Wg"].float()).to(dtype)
+    _, idx, _ = _check(L, _router(L, adaptive=True, tau=tau), renorm, True, tau)
+    if tau == 0.0:
+        assert (idx[:, 1] == -1).all()
+    if tau == 2.0:
+        assert (idx >= 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("adaptive", [False, True])
+@pytest.mark.parametrize("T,D,H,E,r,q,h", [(1, 384, 1536, 8, 128, 32, 64), (19, 72, 264, 5, 24, 8, 30), (5, 70, 301, 4, 20, 9, 33)])
+def test_mlp_router(T, D, H, E, r, q, h, adaptive, dtype):
+    L = _layer(T, D, H, E, 2, r, q, dtype, T + D, mlp=h)
+    tau = 0.5 if adaptive else 0.0
+    _check(L, _router(L, adaptive=adaptive, tau=tau), 1, adaptive, tau)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_routes_as_the_layer_does(dtype):
+    """Equal logits take the lower index, and the routing is route_ex's."""
+    L = _layer(16, 64, 128, 6, 3, 16, 8, dtype, 3)
+    L["Wg"][3] = L["Wg"][1]
+    L["Wg"][5] = L["Wg"][1]
+    L["bg"][:] = 0.25
+    rt = _router(L)
+    _, idx, gate = _few(L, rt)
+    want, wgate = cm.route_ex(L["x"], rt, 6, 3)
+    assert torch.equal(idx, want)
+    assert (gate - wgate).abs().max() <= 2e-5        # route_ex's gates may come from float32 logits
+    order = idx.cpu()
+    for t in range(16):
+        same = [int(e) for e in order[t] if int(e) in (1, 3, 5)]
+        assert same == [1, 3, 5][:len(same)]
+
+
+def test_like_the_layer_for_many_tokens():
+    """Against ffn_forward_ex, whose z, t and u are rounded to bfloat16."""
+    L = _layer(48, 384, 1536, 8, 2, 128, 32, BF16, 8)
+    rt = _router(L)
+    y, idx, _ = _few(L, rt)
+    i2 = torch.empty_like(idx)
+    y2 = cm.ffn_forward_ex(L["x"], L["W1"], L["b1"], L["US"], L["Vt"], L["b2"], L["P"], L["Q"], rt, 2, idx_out=i2)
+    assert torch.equal(idx, i2)
+    assert (y.double() - y2.double()).norm() <= 2e-2 * y2.double().norm()
+
+
+def test_no_biases_and_no_routing_outputs():
+    L = _layer(3, 128, 256, 4, 2, 32, 8, BF16, 4)
+    L["b1"].zero_(), L["b2"].zero_(), L["bg"].zero_()
+    want, _, _ = _few(L, _router(L))
+    y = cm.ffn_forward_few(L["x"], L["W1"], None, L["US"], L["Vt"], None, L["P"], L["Q"], cm.make_router(L["Wg"]), 2)
+    assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("which", ["x", "W1", "US", "Vt", "P", "Q", "Wg", "y"])
+def test_tensors_off_16_byte_boundaries(which, dtype):
+    """Any one tensor at an element boundary: the same numbers."""
+    L = _layer(6, 64, 128, 4, 2, 16, 8, dtype, 5)
+    out = torch.empty(6 * 64 + 1, dtype=dtype, device="cuda")
+    kw = {}
+    if which == "y":
+        kw["out"] = out[1:].view(6, 64)
+    else:
+        t = L[which]
+        flat = torch.empty(t.numel() + 1, dtype=dtype, device="cuda")
+        flat[1:] = t.reshape(-1)
+        L[which] = flat[1:].view(t.shape)
+        assert L[which].data_ptr() % 16 != 0
+    _check(L, _router(L), **kw)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_bad_tokens_stay_alone(dtype):
+    """NaN, infinities and the type's largest values in some tokens leave the
+    others as they were; a choice is made for every token."""
+    L = _layer(20, 64, 160, 5, 2, 24, 8, dtype, 6)
+    rt = _router(L)
+    want, widx, wgate = _few(L, rt)
+    L["x"][2] = float("nan")
+    L["x"][5, 7] = float("inf")
+    L["x"][17] = torch.finfo(dtype).max
+    y, idx, gate = _few(L, rt)
+    keep = [t for t in range(20) if t not in (2, 5, 17)]
+    assert torch.equal(y[keep], want[keep]) and torch.equal(idx[keep], widx[keep])
+    assert torch.equal(gate[keep], wgate[keep])
+    assert ((idx >= 0) & (idx < 5)).all() and (idx[:, 0] != idx[:, 1]).all()
+    assert y[2].isnan().all() and not y[5].isfinite().any()
+
+
+def test_large_activations_do_not_break_the_two_parts_of_z():
+    """bfloat16 z far from one: its rounded part and the rest stay finite."""
+    L = _layer(2, 32, 64, 2, 1, 16, 8, BF16, 9)
+    L["x"] *= 2.0 ** 100
+    L["Wg"][0] = 0
+    L["Wg"][1] = 0
+    L["b1"].zero_(), L["b2"].zero_()
+    _check(L, _router(L))
+
+
+def test_streams_graphs_and_a_shared_workspace():
+    """Two captured graphs over one workspace, on another stream, replayed with
+    new inputs and eager calls between: the eager results, every time."""
+    A, B = _layer(1, 384, 1536, 8, 2, 128, 32, BF16, 1), _layer(12, 384, 1536, 8, 2, 128, 32, BF16, 2)
+    n = max(cm.few_workspace_bytes(cm.make_shape(t, 384, 8, 2, cm.BF16, H=1536, r=128, q=32)) for t in (1, 12))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    ra, rb = _router(A), _router(B, adaptive=True, tau=0.4)
+    stream, graphs = torch.cuda.Stream(), []
+    stream.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for L, rt in ((A, ra), (B, rb)):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            graphs.append((g, _few(L, rt, ws=ws)))
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    for i in range(4):
+        for (g, got), (L, rt) in zip(graphs, ((A, ra), (B, rb))):
+            L["x"].copy_(torch.randn(L["x"].shape, device="cuda", generator=gen))
+            want = _few(L, rt)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(got, want):
+                assert torch.equal(a, b), i
+
+
+def test_no_tokens_and_too_many():
+    L = _layer(65, 64, 128, 4, 2, 16, 8, BF16, 7)
+    rt = _router(L)
+    with pytest.raises(cm.ClearMoEError):
+        _few(L, rt)
+    L["x"] = L["x"][:0]
+    y, _, _ = _few(L, rt)
+    assert y.shape == (0, 64)
+    L = _layer(4, 64, 128, 4, 2, 16, 8, BF16, 7)
+    W2 = torch.zeros(64, 128, dtype=BF16, device="cuda")
+    with pytest.raises(cm.ClearMoEError, match="unsupported"):
+        _few(L, cm.make_router(L["Wg"], L["bg"], dense_stride=2, W2=W2))

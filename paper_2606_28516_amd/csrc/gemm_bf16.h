@@ -90,16 +90,6 @@ __device__ __forceinline__ uint32_t gb_b_offset(const GemmDesc& g, const GbParts
                     : kGbOob;
 }
 
-template <int TM, int TN>
-__device__ __forceinline__ void gb_zero(f32x16 (&acc)[TM][TN]) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-}
-
 // Bias of column nw + lane (nw: the wave's first column; 0 past N or without a
 // bias), loaded before the k loop and added after it: a register a lane in
 // between.  An accumulator that starts at the bias rounds every partial sum

@@ -163,9 +163,304 @@ hipError_t q8_rows(const Q8Desc& g, hipStream_t st) {
     return hipGetLastError();
 }
 
+// ---------------------------------------------------------------------------
+// Many rows: tiles through LDS.
+// ---------------------------------------------------------------------------
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Bytes to the LDS rows of a tile: a stage is 128 bytes (one scale block) of
+// k, so a stage row is a whole line and its scale one byte.
+__device__ __forceinline__ i32x8 q8_lds_frag(const unsigned char* p, uint32_t off) {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(p + off), b = *reinterpret_cast<const u32x4*>(p + (off ^ 16u));
+    i32x8 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = static_cast<int>(a[i]);
+        f[i + 4] = static_cast<int>(b[i]);
+    }
+    return f;
+}
+
+// Epilogue of one wave: 32 TM rows from rw, the 128 columns of scale block
+// blk.  Lane l holds row i * 32 + l % 32 and, for each half h of a tile's 16
+// values, eight consecutive columns (gb_col_of_slot).  Rows are rounded, put
+// together in 32 rows of this wave's own LDS and stored as whole row pieces.
+// b0, b1: the bias of columns lane and 64 + lane.
+template <int TM, int OUT>
+__device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, int rw, int blk, int lane,
+                                            unsigned char* wb, bool nt, float b0, float b1, f32x16 (&acc)[TM][4]) {
+    constexpr int RB = OUT == kQ8OutBf16 ? 256 : 128, CH = RB / 16, RPI = 64 / CH;
+    const int lrow = lane & 31, lh = lane >> 5, nw = blk * kQ8Block;
+    reinterpret_cast<float*>(wb)[lane] = b0;
+    reinterpret_cast<float*>(wb)[64 + lane] = b1;
+    __builtin_amdgcn_wave_barrier();
+    f32x4 bias[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            bias[j][h] = *reinterpret_cast<const f32x4*>(wb + 4 * (j * 32 + 16 * (h >> 1) + 8 * lh + 4 * (h & 1)));
+    __builtin_amdgcn_wave_barrier();
+    const int cols = static_cast<int>(q8_cols(g.N));
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] += bias[j][v >> 2][v & 3];
+        if (g.gelu)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = gelu_erf(acc[i][j][v]);
+        if constexpr (OUT == kQ8OutBf16) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x4 w;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        w[q] = pack2_bf16(acc[i][j][8 * h + 2 * q], acc[i][j][8 * h + 2 * q + 1]);
+                    const int ch = j * 4 + 2 * h + lh;
+                    *reinterpret_cast<u32x4*>(wb + lrow * RB + ((ch ^ (lrow % CH)) << 4)) = w;
+                }
+        } else {
+            constexpr int FMT = OUT == kQ8OutE4M3 ? kQ8E4M3 : kQ8E5M2;
+            // a lane and the one 32 further hold a row's block; infinities
+            // (rare: the whole wave looks again) do not set the scale
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) m = fmaxf(m, fabsf(acc[i][j][v]));
+            if (__ballot(!(m < __builtin_inff())) != 0) {
+                m = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) m = fmaxf(m, q8_mag(acc[i][j][v]));
+            }
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const int e = q8_exponent(__float_as_uint(m), q8_top_exp(FMT));
+            const float k = q8_two_to(-e);
+            const int rl = rw + i * 32 + lrow;
+            if (lh == 0 && rl < t.rows) {
+                uint8_t* s = g.SC + (t.m_lo + rl) * g.sc_ld;
+                s[blk] = static_cast<uint8_t>(e + kQ8One);
+                if (nw + kQ8Block >= g.N)                       // the last block fills the row up
+                    for (int64_t p = blk + 1; p < g.sc_ld; ++p) s[p] = kQ8One;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x2 w;
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int v = 8 * h + 4 * q;
+                        w[q] = q8_pack4<FMT>(acc[i][j][v] * k, acc[i][j][v + 1] * k, acc[i][j][v + 2] * k,
+                                             acc[i][j][v + 3] * k);
+                    }
+                    const int ch = j * 2 + h;
+                    *reinterpret_cast<u32x2*>(wb + lrow * RB + ((ch ^ (lrow % CH)) << 4) + 8 * lh) = w;
+                }
+        }
+        // one wave's LDS accesses complete in order: only the compiler has to
+        // keep them in place
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int it = 0; it < 32 / RPI; ++it) {
+            const int rr = it * RPI + lane / CH, ch = lane % CH;
+            const u32x4 w = *reinterpret_cast<const u32x4*>(wb + rr * RB + ((ch ^ (rr % CH)) << 4));
+            const int rl = rw + i * 32 + rr;
+            if (rl >= t.rows) continue;
+            if constexpr (OUT == kQ8OutBf16) {
+                const int n = nw + ch * 8;
+                bf16_bits* c = static_cast<bf16_bits*>(g.C) + (t.m_lo + rl) * g.ldc + n;
+                if (g.wide) {
+                    if (n < g.N) gb_store(reinterpret_cast<u32x4*>(c), w, nt);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (n + q < g.N) c[q] = static_cast<bf16_bits>(w[q >> 1] >> (16 * (q & 1)));
+                }
+            } else {
+                const int n = nw + ch * 16;
+                if (n < cols)
+                    gb_store(reinterpret_cast<u32x4*>(static_cast<uint8_t*>(g.C) + (t.m_lo + rl) * g.ldc + n), w, nt);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Bias of columns c + lane and c + 64 + lane (0 past N or without one).
+__device__ __forceinline__ void q8_bias(const Q8Desc& g, int seg, int c, int lane, float& b0, float& b1) {
+    const float* p = g.bias != nullptr ? g.bias + static_cast<int64_t>(seg) * g.N : nullptr;
+    const __amdgpu_buffer_rsrc_t rb = raw_rsrc(p, p != nullptr ? static_cast<int64_t>(g.N) * 4 : 0);
+    b0 = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, (c + lane) * 4, 0, 0));
+    b1 = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, (c + 64 + lane) * 4, 0, 0));
+}
+
+// 256 x 128 tile over four waves (64 x 128 each), two workgroups on a CU, so
+// that one's epilogue runs beside the other's matrix instructions.  80 KB of
+// LDS each: A has two stage buffers, B one, which is free as soon as its
+// fragments are in registers.
+template <int FA, int FB, int OUT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
+    constexpr int SB = kGbRow, BM = 256, BN = kQ8Block, CPR = 8, BK = kQ8Block, TM = 2, TN = 4, AL = 8, BL = 4;
+    constexpr int ABUF = BM * SB, BOFF = 2 * ABUF;      // buffers A0 A1 B
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[BOFF + BN * SB];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lrow = lane & 31, lh = lane >> 5;
+
+    GbTile t;
+    if (!gb_tile<BM>(g, mtiles, ntiles, group, lane, t)) return;
+    const int n0 = t.nt * BN, K = g.K;
+    const int lr = lane / CPR, cp = lane % CPR;
+    // first k of the lane's chunk in an even load's 8 rows; odd: ^ 64
+    const int kc0 = 16 * (cp ^ (lr >> 1));
+    const gb_i32x4 da = gb_desc(g.A + t.m_lo * g.lda, (static_cast<int64_t>(t.rows) - 1) * g.lda + K);
+    const int nrows = g.N - n0 < BN ? g.N - n0 : BN;
+    const gb_i32x4 db = gb_desc(g.B + t.seg * g.b_seg_stride + static_cast<int64_t>(n0) * K,
+                                static_cast<int64_t>(nrows) * K);
+    // Load i brings the rows (8 i + lr) of the wave: byte offsets of its first
+    // (even) load, to which i adds whole rows; rows past the tile's lie past
+    // the descriptor's end and read zeros.
+    const uint32_t lda = static_cast<uint32_t>(g.lda);
+    const uint32_t va = static_cast<uint32_t>(wave * AL * 8 + lr) * lda, vb = static_cast<uint32_t>((wave * BL * 8 + lr) * K);
+    const int nk = static_cast<int>(q8_blocks(K));
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(
+        static_cast<uint32_t>(reinterpret_cast<uintptr_t>((gb_lds_u32*)smem)));
+    auto dma_a = [&](int kt, int b) {
+        const bool cut = (kt + 1) * BK > K;             // uniform: chunks past the end read zeros
+#pragma unroll
+        for (int i = 0; i < AL; ++i) {
+            const int kc = kc0 ^ (64 * (i & 1));
+            uint32_t v = va + static_cast<uint32_t>(8 * i) * lda + kc;
+            if (cut) v = kt * BK + kc < K ? v : kGbOob;
+            gb_dma16(da, v, __builtin_amdgcn_readfirstlane(kt * BK),
+                     __builtin_amdgcn_readfirstlane(lds0 + b * ABUF + (wave * AL + i) * 1024));
+        }
+    };
+    auto dma_b = [&](int kt) {
+        const bool cut = (kt + 1) * BK > K;
+#pragma unroll
+        for (int i = 0; i < BL; ++i) {
+            const int kc = kc0 ^ (64 * (i & 1));
+            uint32_t v = vb + static_cast<uint32_t>(8 * i * K) + kc;
+            if (cut) v = kt * BK + kc < K ? v : kGbOob;
+            gb_dma16(db, v, __builtin_amdgcn_readfirstlane(kt * BK),
+                     __builtin_amdgcn_readfirstlane(lds0 + BOFF + (wave * BL + i) * 1024));
+        }
+    };
+    // scales: a word holds those of four stages (rows past the tile's: 0)
+    const __amdgpu_buffer_rsrc_t ra = raw_rsrc(g.SA + t.m_lo * g.sa_ld, static_cast<int64_t>(t.rows) * g.sa_ld);
+    const uint32_t vs = static_cast<uint32_t>(wave * 64 + lrow) * static_cast<uint32_t>(g.sa_ld);
+    const uint8_t* psb = g.SB + t.seg * g.sb_seg_stride + static_cast<int64_t>(t.nt) * g.sb_ld;
+    uint32_t sa[TM], sb;
+    auto scales = [&](int kt) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+            sa[i] = static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b32(
+                ra, static_cast<int>(vs + static_cast<uint32_t>(i * 32) * static_cast<uint32_t>(g.sa_ld)), kt, 0));
+        sb = *reinterpret_cast<const uint32_t*>(psb + kt);
+    };
+    scales(0);
+    dma_a(0, 0);
+    dma_b(0);
+    f32x16 acc[TM][TN];
+    gb_zero(acc);
+
+    const int bcol = gb_col_of_slot(lrow);
+    uint32_t oa[2], ob[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        oa[s] = static_cast<uint32_t>((wave * 64 + lrow) * SB + (((4 * s + 2 * lh) ^ gb_swz<SB>(lrow)) << 4));
+        ob[s] = static_cast<uint32_t>(BOFF + bcol * SB + (((4 * s + 2 * lh) ^ gb_swz<SB>(bcol)) << 4));
+    }
+    i32x8 fa[2][TM], fb[2][TN];
+    auto read_a = [&](int b, int s) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[s][i] = q8_lds_frag(smem + b * ABUF + i * 32 * SB, oa[s]);
+    };
+    auto read_b = [&](int s) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[s][j] = q8_lds_frag(smem + j * 32 * SB, ob[s]);
+    };
+    auto mm = [&](int s, int kt) {
+        const int sh = 8 * (kt & 3);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                    fb[s][j], fa[s][i], acc[i][j], FB, FA, 0, static_cast<int>(sb >> sh), 0,
+                    static_cast<int>(sa[i] >> sh));
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int k0 = 0; k0 < nk; k0 += 2) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int kt = k0 + b;
+            if (kt >= nk) break;
+            // stage kt has landed for every wave, and every wave is done
+            // reading the other A buffer
+            gb_wait_barrier<0>();
+            if ((kt & 3) == 0) {
+                // the words of these four stages have landed too: take them
+                // before the next loads are issued, so that nothing waits
+                // for those
+#pragma unroll
+                for (int i = 0; i < TM; ++i) asm volatile("" : "+v"(sa[i]));
+            }
+            if (kt + 1 < nk) dma_a(kt + 1, b ^ 1);
+            read_b(0);
+            read_a(b, 0);
+            read_b(1);
+            mm(0, kt);
+            if (kt + 1 < nk) {
+                // every wave has read this stage's B
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                dma_b(kt + 1);
+            }
+            read_a(b, 1);
+            mm(1, kt);
+            if ((kt & 3) == 3 && kt + 1 < nk) scales(kt + 1);
+        }
+    }
+    gb_wait_barrier<0>();                        // the stage buffers are free
+    float b0, b1;                                // (the other workgroup runs while they come)
+    q8_bias(g, t.seg, n0, lane, b0, b1);
+    q8_epilogue<TM, OUT>(g, t, wave * 64, t.nt, lane, smem + wave * (32 * 256), nt_store != 0, b0, b1, acc);
+}
+
+// Results of 16 MB or more are written past the L2.
+constexpr int64_t kQ8StreamBytes = 16 << 20;
+
+template <int FA, int FB, int OUT>
+hipError_t q8_duo(const Q8Desc& g, hipStream_t st) {
+    const int64_t mt = (g.M + 255) / 256 + (g.seg_offsets != nullptr ? g.nseg : 0);
+    const int64_t nt = q8_blocks(g.N);
+    const int64_t grid = (mt * nt + kGbXcds - 1) / kGbXcds * kGbXcds;
+    const int64_t bytes = g.M * g.N * (OUT == kQ8OutBf16 ? 2 : 1);
+    launch_kernel(k_q8_duo<FA, FB, OUT>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, g,
+                  static_cast<int>(mt), static_cast<int>(nt), 4, bytes >= kQ8StreamBytes ? 1 : 0);
+    return hipGetLastError();
+}
+
 template <int FA, int FB>
 hipError_t q8_formats(const Q8Desc& g, hipStream_t st) {
     if (g.out == kQ8OutF32) return q8_rows<FA, FB, 1, 8, true>(g, st);
+    if (g.M > 64) {
+        if (g.out == kQ8OutBf16) return q8_duo<FA, FB, kQ8OutBf16>(g, st);
+        return g.out == kQ8OutE4M3 ? q8_duo<FA, FB, kQ8OutE4M3>(g, st) : q8_duo<FA, FB, kQ8OutE5M2>(g, st);
+    }
     if (g.out == kQ8OutBf16) return q8_rows<FA, FB, 1, 8, false>(g, st);
     return q8_rows<FA, FB, 8, 2, false>(g, st);
 }

@@ -152,6 +152,16 @@ __device__ __forceinline__ bool gb_tile(const Desc& g, int mtiles, int ntiles, i
     return true;
 }
 
+template <int TM, int TN>
+__device__ __forceinline__ void gb_zero(f32x16 (&acc)[TM][TN]) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+}
+
 }  // namespace
 
 }  // namespace clearmoe

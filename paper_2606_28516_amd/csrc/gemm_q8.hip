@@ -181,38 +181,88 @@ __device__ __forceinline__ i32x8 q8_lds_frag(const unsigned char* p, uint32_t of
     return f;
 }
 
+// GELU for results that are rounded to 8 bits or bfloat16: v Phi(v) =
+// max(v, 0) - |v| Phi(-|v|) with Phi(-a) = 2^P(a), P the polynomial of degree
+// 7 that is nearest to log2 Phi(-a) on [0, 6] (4.7e-6, so GELU is off by at
+// most 3.3e-6 of itself there; further out P falls on without end): 13
+// full-rate operations' time instead of gelu_erf's 20.  fc1 + GELU over many
+// rows is bound by this vector work.
+__device__ __forceinline__ float q8_gelu(float v) {
+    const float a = fabsf(v);
+    float p = __builtin_fmaf(a, -1.83535093e-06f, 6.16087855e-05f);
+    p = __builtin_fmaf(a, p, -9.3060248e-04f);
+    p = __builtin_fmaf(a, p, 8.50815862e-03f);
+    p = __builtin_fmaf(a, p, -5.39604758e-02f);
+    p = __builtin_fmaf(a, p, -4.58464246e-01f);
+    p = __builtin_fmaf(a, p, -1.15125091f);
+    p = __builtin_fmaf(a, p, -9.99995318e-01f);
+    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), fmaxf(v, 0.0f));
+}
+
+// Four floats over a scale -> four bytes (as q8_pack4, the division inside).
+template <int FMT>
+__device__ __forceinline__ uint32_t q8_pack4_over(float a, float b, float c, float d, float scale) {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    s16x2 v = {0, 0};
+    if constexpr (FMT == kQ8E4M3) {
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, a, b, scale, false);
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, c, d, scale, true);
+    } else {
+        v = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(v, a, b, scale, false);
+        v = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(v, c, d, scale, true);
+    }
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// Sums of a wave's 32 TM rows x 128 columns from c start at the bias, which
+// saves an addition a value at the end; it is put in the lanes' order through
+// 512 bytes of this wave's own LDS.
+template <int TM>
+__device__ __forceinline__ void q8_start(const Q8Desc& g, int seg, int c, int lane, unsigned char* wb,
+                                         f32x16 (&acc)[TM][4]) {
+    if (g.bias == nullptr) {
+        gb_zero(acc);
+        return;
+    }
+    const float* p = g.bias + static_cast<int64_t>(seg) * g.N;
+    const __amdgpu_buffer_rsrc_t rb = raw_rsrc(p, static_cast<int64_t>(g.N) * 4);
+    const int lh = lane >> 5;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        reinterpret_cast<float*>(wb)[h * 64 + lane] =
+            __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, (c + h * 64 + lane) * 4, 0, 0));
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const f32x4 b =
+                *reinterpret_cast<const f32x4*>(wb + 4 * (j * 32 + 16 * (h >> 1) + 8 * lh + 4 * (h & 1)));
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][j][4 * h + v] = b[v];
+        }
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Epilogue of one wave: 32 TM rows from rw, the 128 columns of scale block
 // blk.  Lane l holds row i * 32 + l % 32 and, for each half h of a tile's 16
 // values, eight consecutive columns (gb_col_of_slot).  Rows are rounded, put
 // together in 32 rows of this wave's own LDS and stored as whole row pieces.
-// b0, b1: the bias of columns lane and 64 + lane.
 template <int TM, int OUT>
 __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, int rw, int blk, int lane,
-                                            unsigned char* wb, bool nt, float b0, float b1, f32x16 (&acc)[TM][4]) {
+                                            unsigned char* wb, bool nt, f32x16 (&acc)[TM][4]) {
     constexpr int RB = OUT == kQ8OutBf16 ? 256 : 128, CH = RB / 16, RPI = 64 / CH;
     const int lrow = lane & 31, lh = lane >> 5, nw = blk * kQ8Block;
-    reinterpret_cast<float*>(wb)[lane] = b0;
-    reinterpret_cast<float*>(wb)[64 + lane] = b1;
-    __builtin_amdgcn_wave_barrier();
-    f32x4 bias[4][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int h = 0; h < 4; ++h)
-            bias[j][h] = *reinterpret_cast<const f32x4*>(wb + 4 * (j * 32 + 16 * (h >> 1) + 8 * lh + 4 * (h & 1)));
-    __builtin_amdgcn_wave_barrier();
     const int cols = static_cast<int>(q8_cols(g.N));
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] += bias[j][v >> 2][v & 3];
         if (g.gelu)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][j][v] = gelu_erf(acc[i][j][v]);
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = q8_gelu(acc[i][j][v]);
         if constexpr (OUT == kQ8OutBf16) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -243,7 +293,7 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
             }
             m = fmaxf(m, __shfl_xor(m, 32));
             const int e = q8_exponent(__float_as_uint(m), q8_top_exp(FMT));
-            const float k = q8_two_to(-e);
+            const float k = q8_two_to(e);
             const int rl = rw + i * 32 + lrow;
             if (lh == 0 && rl < t.rows) {
                 uint8_t* s = g.SC + (t.m_lo + rl) * g.sc_ld;
@@ -259,8 +309,8 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         const int v = 8 * h + 4 * q;
-                        w[q] = q8_pack4<FMT>(acc[i][j][v] * k, acc[i][j][v + 1] * k, acc[i][j][v + 2] * k,
-                                             acc[i][j][v + 3] * k);
+                        w[q] = q8_pack4_over<FMT>(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2],
+                                                  acc[i][j][v + 3], k);
                     }
                     const int ch = j * 2 + h;
                     *reinterpret_cast<u32x2*>(wb + lrow * RB + ((ch ^ (lrow % CH)) << 4) + 8 * lh) = w;
@@ -293,14 +343,6 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
         }
         __builtin_amdgcn_wave_barrier();
     }
-}
-
-// Bias of columns c + lane and c + 64 + lane (0 past N or without one).
-__device__ __forceinline__ void q8_bias(const Q8Desc& g, int seg, int c, int lane, float& b0, float& b1) {
-    const float* p = g.bias != nullptr ? g.bias + static_cast<int64_t>(seg) * g.N : nullptr;
-    const __amdgpu_buffer_rsrc_t rb = raw_rsrc(p, p != nullptr ? static_cast<int64_t>(g.N) * 4 : 0);
-    b0 = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, (c + lane) * 4, 0, 0));
-    b1 = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, (c + 64 + lane) * 4, 0, 0));
 }
 
 // 256 x 128 tile over four waves (64 x 128 each), two workgroups on a CU, so
@@ -374,7 +416,8 @@ void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
     dma_a(0, 0);
     dma_b(0);
     f32x16 acc[TM][TN];
-    gb_zero(acc);
+    // (through the second buffer of A, which is filled after the first wait)
+    q8_start<TM>(g, t.seg, n0, lane, smem + ABUF + wave * 512, acc);
 
     const int bcol = gb_col_of_slot(lrow);
     uint32_t oa[2], ob[2];
@@ -435,9 +478,7 @@ void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
         }
     }
     gb_wait_barrier<0>();                        // the stage buffers are free
-    float b0, b1;                                // (the other workgroup runs while they come)
-    q8_bias(g, t.seg, n0, lane, b0, b1);
-    q8_epilogue<TM, OUT>(g, t, wave * 64, t.nt, lane, smem + wave * (32 * 256), nt_store != 0, b0, b1, acc);
+    q8_epilogue<TM, OUT>(g, t, wave * 64, t.nt, lane, smem + wave * (32 * 256), nt_store != 0, acc);
 }
 
 // Results of 16 MB or more are written past the L2.

@@ -127,10 +127,14 @@ def _sum_bound(K, mass, wide):
     return ((K + 8) * 2.0 ** -23 + (0.0 if wide else 2.0 ** -10)) * mass
 
 
-def _gelu_bound(v, d):
-    """Error of the float32 GELU of a sum v that is off by d: slope at most
-    1.13, the erf's 1.5e-7 and a few roundings."""
-    return 1.13 * d + 4e-7 * v.abs()
+def _gelu_bound(v, d, wide):
+    """Error of the GELU of a sum v that is off by d: slope at most 1.13, and
+    its own error: the erf's 1.5e-7 and a few roundings for float32 results;
+    otherwise that of a polynomial for log2 Phi(-|v|), 4.7e-6 ln 2 = 3.3e-6 of
+    |v| Phi(-|v|) up to |v| = 6 (further out that is below 6e-9), and the
+    roundings of the exponent, seven terms below 64: 7 * 64 * 2^-24 ln 2 of
+    |v| Phi(-|v|) <= |v| / 2, less than 1e-5 |v|."""
+    return 1.13 * d + (4e-7 * v.abs() if wide else 1.4e-5 * v.abs() + 1e-8)
 
 
 # The share of _sum_bound that seven cut products in eight leave on average:
@@ -160,7 +164,7 @@ def _reference(a, b, bias, offsets, gelu, wide):
     d = _sum_bound(K, mass, wide)
     mean = (math.sqrt(K) + 8) * 2.0 ** -23 * mass + (0.0 if wide else CUT) * sq
     if gelu:
-        return _gelu(y), _gelu_bound(y, d), _gelu_bound(y, mean), live
+        return _gelu(y), _gelu_bound(y, d, wide), _gelu_bound(y, mean, wide), live
     return y, d, mean, live
 
 
@@ -337,7 +341,7 @@ def _ffn_reference(x, w1, b1, w2, b2, D, H, half):
     pre = xq @ w1.T + b1
     mass = xq.abs() @ w1.abs().T + b1.abs()
     z = _gelu(pre)
-    dz = _gelu_bound(pre, _sum_bound(D, mass, False))
+    dz = _gelu_bound(pre, _sum_bound(D, mass, False), False)
     zp = torch.zeros(T, up(H, 128), dtype=torch.float64)
     zp[:, :H] = z.abs() + dz
     zs = torch.ldexp(torch.ones(T, zp.shape[1] // 128, dtype=torch.float64),

@@ -196,7 +196,9 @@ __device__ __forceinline__ float q8_gelu(float v) {
     p = __builtin_fmaf(a, p, -4.58464246e-01f);
     p = __builtin_fmaf(a, p, -1.15125091f);
     p = __builtin_fmaf(a, p, -9.99995318e-01f);
-    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), fmaxf(v, 0.0f));
+    float m;                                     // (fmaxf takes two instructions: it quiets NaN first)
+    asm("v_max_f32 %0, 0, %1" : "=v"(m) : "v"(v));
+    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), m);
 }
 
 // Four floats over a scale -> four bytes (as q8_pack4, the division inside).
@@ -370,35 +372,37 @@ void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
     const int nrows = g.N - n0 < BN ? g.N - n0 : BN;
     const gb_i32x4 db = gb_desc(g.B + t.seg * g.b_seg_stride + static_cast<int64_t>(n0) * K,
                                 static_cast<int64_t>(nrows) * K);
-    // Load i brings the rows (8 i + lr) of the wave: byte offsets of its first
-    // (even) load, to which i adds whole rows; rows past the tile's lie past
-    // the descriptor's end and read zeros.
+    // Load i brings the rows 8 i + lr of the wave.  Kept are the byte offsets
+    // of the first even and odd one, to which i adds whole rows; rows past the
+    // tile's lie past the descriptor's end and read zeros.  Of the last stage
+    // of a k that ends inside it, chunks past the end get an offset past
+    // everything.
     const uint32_t lda = static_cast<uint32_t>(g.lda);
-    const uint32_t va = static_cast<uint32_t>(wave * AL * 8 + lr) * lda, vb = static_cast<uint32_t>((wave * BL * 8 + lr) * K);
-    const int nk = static_cast<int>(q8_blocks(K));
+    const int nk = static_cast<int>(q8_blocks(K)), left = K - (nk - 1) * BK;
+    uint32_t va[2], vb[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        va[p] = static_cast<uint32_t>(wave * AL * 8 + lr) * lda + (kc0 ^ (64 * p));
+        vb[p] = static_cast<uint32_t>((wave * BL * 8 + lr) * K + (kc0 ^ (64 * p)));
+    }
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(
         static_cast<uint32_t>(reinterpret_cast<uintptr_t>((gb_lds_u32*)smem)));
+    auto first = [&](const uint32_t (&v)[2], int kt, int p) {
+        return kt == nk - 1 && (kc0 ^ (64 * p)) >= left ? kGbOob : v[p];
+    };
     auto dma_a = [&](int kt, int b) {
-        const bool cut = (kt + 1) * BK > K;             // uniform: chunks past the end read zeros
+        const uint32_t v[2] = {first(va, kt, 0), first(va, kt, 1)};
 #pragma unroll
-        for (int i = 0; i < AL; ++i) {
-            const int kc = kc0 ^ (64 * (i & 1));
-            uint32_t v = va + static_cast<uint32_t>(8 * i) * lda + kc;
-            if (cut) v = kt * BK + kc < K ? v : kGbOob;
-            gb_dma16(da, v, __builtin_amdgcn_readfirstlane(kt * BK),
+        for (int i = 0; i < AL; ++i)
+            gb_dma16(da, v[i & 1] + static_cast<uint32_t>(8 * i) * lda, __builtin_amdgcn_readfirstlane(kt * BK),
                      __builtin_amdgcn_readfirstlane(lds0 + b * ABUF + (wave * AL + i) * 1024));
-        }
     };
     auto dma_b = [&](int kt) {
-        const bool cut = (kt + 1) * BK > K;
+        const uint32_t v[2] = {first(vb, kt, 0), first(vb, kt, 1)};
 #pragma unroll
-        for (int i = 0; i < BL; ++i) {
-            const int kc = kc0 ^ (64 * (i & 1));
-            uint32_t v = vb + static_cast<uint32_t>(8 * i * K) + kc;
-            if (cut) v = kt * BK + kc < K ? v : kGbOob;
-            gb_dma16(db, v, __builtin_amdgcn_readfirstlane(kt * BK),
+        for (int i = 0; i < BL; ++i)
+            gb_dma16(db, v[i & 1] + static_cast<uint32_t>(8 * i * K), __builtin_amdgcn_readfirstlane(kt * BK),
                      __builtin_amdgcn_readfirstlane(lds0 + BOFF + (wave * BL + i) * 1024));
-        }
     };
     // scales: a word holds those of four stages (rows past the tile's: 0)
     const __amdgpu_buffer_rsrc_t ra = raw_rsrc(g.SA + t.m_lo * g.sa_ld, static_cast<int64_t>(t.rows) * g.sa_ld);

@@ -320,7 +320,7 @@ int clearmoe_dense_ffn_forward(const clearmoe_shape* shape, const void* x, const
  *     CLEARMOE_ERR_UNSUPPORTED).  Linear routers run inside the first kernel,
  *     every logit in double; an MLP router runs before it, as
  *     clearmoe_route_ex.
- *   - Any D, H, r, q (r + k q <= 16384, else CLEARMOE_ERR_UNSUPPORTED); where
+ *   - Any D, H, r, q (r + k q <= 12288, else CLEARMOE_ERR_UNSUPPORTED); where
  *     all are multiples of 8 (bf16) or 4 (float32) and every tensor is 16-byte
  *     aligned, memory is read in 16-byte pieces, else element by element, for
  *     which element alignment is enough (an MLP router's weights keep the

@@ -192,6 +192,29 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    """_p as a plain address: ctypes turns it into the pointer argument."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ClearMoEError("tensor is not on the GPU")
+    if not t.is_contiguous():
+        raise ClearMoEError("tensor is not contiguous")
+    return t.data_ptr()
+
+
+def _queue(x: torch.Tensor, stream) -> int:
+    """The stream of a call on x's device, which has to be the current one: the
+    kernels are launched there.  The current stream is asked for by its handle
+    (a torch.cuda.Stream object costs 3 us, a quarter of a small call)."""
+    dev = x.get_device()
+    if dev != torch.cuda.current_device():
+        raise ClearMoEError("the tensors are not on the current device")
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
 def make_shape(T, D, E, k, dtype, H=0, r=0, q=0, renorm=1) -> Shape:
     """renorm = 1: the top-k gates renormalised over the selected experts;
     0: their probabilities under the softmax over all E."""
@@ -437,13 +460,13 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
     tokens, with any router without class tokens.  Returns y."""
     T, D = x.shape
     E, _, q = P.shape
-    s = make_shape(T, D, E, k, _dt(x), H=W1.shape[0], r=US.shape[1], q=q, renorm=renorm)
+    s = Shape(T, D, W1.shape[0], E, k, US.shape[1], q, _dt(x), renorm)
+    xp, st = _ptr(x), _queue(x, stream)
     ws = alloc_few_workspace(s, x.device) if ws is None else ws
-    y = torch.empty((T, D), dtype=x.dtype, device=x.device) if out is None else out
-    rc = lib().clearmoe_ffn_forward_few(ctypes.byref(s), ctypes.byref(router), _p(x), _p(W1),
-                                        _p(b1), _p(US), _p(Vt), _p(b2), _p(P), _p(Q), _p(y),
-                                        _p(idx_out), _p(gate_out), _p(ws), ws.numel(),
-                                        _stream(stream))
+    y = torch.empty_like(x) if out is None else out
+    rc = lib().clearmoe_ffn_forward_few(ctypes.byref(s), ctypes.byref(router), xp, _ptr(W1),
+                                        _ptr(b1), _ptr(US), _ptr(Vt), _ptr(b2), _ptr(P), _ptr(Q), _ptr(y),
+                                        _ptr(idx_out), _ptr(gate_out), _ptr(ws), ws.numel(), st)
     _check(rc, "clearmoe_ffn_forward_few")
     return y
 
@@ -467,10 +490,15 @@ def _scale_cols(cols: int) -> int:
     return (cols + 511) // 512 * 4
 
 
-def _scales(s: torch.Tensor, shape, what: str) -> ctypes.c_void_p:
-    if s.dtype != torch.float8_e8m0fnu or tuple(s.shape) != tuple(shape):
-        raise ClearMoEError(f"{what} must be float8_e8m0fnu {tuple(shape)}, not {s.dtype} {tuple(s.shape)}")
-    return _p(s)
+def _shaped(t: torch.Tensor, dtype, shape: tuple, what: str) -> int:
+    """The address of a tensor that has to have this type and shape."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ClearMoEError(f"{what} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _shaped_or_none(t: Optional[torch.Tensor], dtype, shape: tuple, what: str) -> Optional[int]:
+    return None if t is None else _shaped(t, dtype, shape, what)
 
 
 def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
@@ -481,21 +509,24 @@ def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
     blocks up to a multiple of 4] in float8_e8m0fnu)."""
     if x.dim() not in (2, 3):
         raise ClearMoEError("quantize takes [rows, cols] or [batch, rows, cols]")
-    batch = x.shape[0] if x.dim() == 3 else 1
-    rows, cols = x.shape[-2:]
-    ldx = x.stride(-2) if rows > 1 else max(cols, 1)
-    if batch > 1 and rows == 1:
-        ldx = x.stride(0)
     if not x.is_cuda:
         raise ClearMoEError("tensor is not on the GPU")
-    if x.numel() > 0 and ((cols > 1 and x.stride(-1) != 1) or (batch > 1 and x.stride(0) != rows * ldx)):
-        raise ClearMoEError("rows must be contiguous and evenly spaced over the batch")
-    lead = tuple(x.shape[:-2])
-    v = torch.empty(lead + (rows, _value_cols(cols)), dtype=fmt, device=x.device)
+    lead = x.shape[:-2]
+    batch = x.shape[0] if lead else 1
+    rows, cols = x.shape[-2:]
+    if x.is_contiguous():
+        ldx = cols
+    else:
+        ldx = x.stride(-2) if rows > 1 else x.stride(0) if batch > 1 else cols
+        if x.numel() > 0 and ((cols > 1 and x.stride(-1) != 1) or (batch > 1 and x.stride(0) != rows * ldx)):
+            raise ClearMoEError("rows must be contiguous and evenly spaced over the batch")
+    st = _queue(x, stream)
+    dt, code = _dt(x), _format(fmt)
     nr = rows if block_rows == 1 else -(-rows // 128)
-    s = torch.empty(lead + (nr, _scale_cols(cols)), dtype=torch.float8_e8m0fnu, device=x.device)
-    rc = lib().clearmoe_quantize(_dt(x), _format(fmt), block_rows, batch, rows, cols,
-                                 ctypes.c_void_p(x.data_ptr()), ldx, _p(v), _p(s), _stream(stream))
+    v = torch.empty((*lead, rows, _value_cols(cols)), dtype=fmt, device=x.device)
+    s = torch.empty((*lead, nr, _scale_cols(cols)), dtype=torch.float8_e8m0fnu, device=x.device)
+    rc = lib().clearmoe_quantize(dt, code, block_rows, batch, rows, cols, x.data_ptr(), ldx, v.data_ptr(),
+                                 s.data_ptr(), st)
     _check(rc, "clearmoe_quantize")
     return v, s
 
@@ -508,28 +539,24 @@ def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offset
     as out had them).  Returns C [M, N] in out_dtype; for an 8-bit out_dtype
     (values [M, N up to a multiple of 16], scales)."""
     M, K = a.shape
-    grouped = offsets is not None
-    E = b.shape[0] if grouped else 0
+    E = 0 if offsets is None else b.shape[0]
+    lead = (E,) if E else ()
     N = b.shape[-2]
-    if b.dim() != (3 if grouped else 2) or b.shape[-1] != K:
-        raise ClearMoEError(f"b must be [{'E, ' if grouped else ''}N, {K}], not {tuple(b.shape)}")
-    lead = (E,) if grouped else ()
-    if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != lead + (N,)):
-        raise ClearMoEError(f"bias must be float32 {lead + (N,)}")
-    if grouped and (offsets.dtype != torch.int32 or tuple(offsets.shape) != (E + 1,)):
-        raise ClearMoEError(f"offsets must be int32 {(E + 1,)}")
+    if b.shape != (*lead, N, K):
+        raise ClearMoEError(f"b must be [{'E, ' if E else ''}N, {K}], not {tuple(b.shape)}")
+    byte = out_dtype in _FORMATS
     if out_dtype not in _OUTS:
         raise ClearMoEError(f"unsupported dtype {out_dtype}")
-    byte = out_dtype in _FORMATS
-    cols = _value_cols(N) if byte else N
+    cols, sc, e8 = _value_cols(N) if byte else N, _scale_cols(K), torch.float8_e8m0fnu
+    p = Product(M, N, K, E, _format(a.dtype), _format(b.dtype), _OUTS[out_dtype], 1 if gelu else 0, 0, 0, 0)
+    args = (_ptr(a), _shaped(a_scale, e8, (M, sc), "a_scale"), _ptr(b),
+            _shaped(b_scale, e8, (*lead, -(-N // 128), sc), "b_scale"),
+            _shaped_or_none(bias, torch.float32, (*lead, N), "bias"),
+            _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets"))
+    st = _queue(a, stream)
     c = torch.empty((M, cols), dtype=out_dtype, device=a.device) if out is None else out
-    if c.dtype != out_dtype or tuple(c.shape) != (M, cols):
-        raise ClearMoEError(f"out must be {out_dtype} {(M, cols)}")
-    cs = torch.empty((M, _scale_cols(N)), dtype=torch.float8_e8m0fnu, device=a.device) if byte else None
-    p = Product(M, N, K, E, _format(a.dtype), _format(b.dtype), _OUTS[out_dtype], int(gelu), 0, 0, 0)
-    rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), _p(a), _scales(a_scale, (M, _scale_cols(K)), "a_scale"),
-                                       _p(b), _scales(b_scale, lead + (-(-N // 128), _scale_cols(K)), "b_scale"),
-                                       _p(bias), _p(offsets), _p(c), _p(cs), _stream(stream))
+    cs = torch.empty((M, _scale_cols(N)), dtype=e8, device=a.device) if byte else None
+    rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), *args, _shaped(c, out_dtype, (M, cols), "out"), _ptr(cs), st)
     _check(rc, "clearmoe_quantized_gemm")
     return (c, cs) if byte else c
 
@@ -550,27 +577,22 @@ def quantized_ffn_forward(x, W1, W1_scale, b1, W2, W2_scale, b2, offsets=None,
     [E + 1], rows sorted by expert through their expert's ([E, H, .],
     [E, D, .]; rows outside all groups are left as out had them)."""
     T, D = x.shape
-    grouped = offsets is not None
-    lead = (W1.shape[0],) if grouped else ()
-    E, H = (lead[0] if grouped else 1), W1.shape[-2]
-    for w, n, kk in ((W1, H, D), (W2, D, H)):
-        if w.dtype != torch.float8_e4m3fn or tuple(w.shape) != lead + (n, _value_cols(kk)):
-            raise ClearMoEError(f"weights must be float8_e4m3fn {lead + (n, _value_cols(kk))}, not "
-                                f"{w.dtype} {tuple(w.shape)}")
-    for b, n in ((b1, H), (b2, D)):
-        if b is not None and (b.dtype != torch.float32 or tuple(b.shape) != lead + (n,)):
-            raise ClearMoEError(f"biases must be float32 {lead + (n,)}")
-    if grouped and (offsets.dtype != torch.int32 or tuple(offsets.shape) != (E + 1,)):
-        raise ClearMoEError(f"offsets must be int32 {(E + 1,)}")
-    s = make_shape(T, D, E, 1, _dt(x), H=H)
+    lead = () if offsets is None else (W1.shape[0],)
+    E, H = (lead[0] if lead else 1), W1.shape[-2]
+    e4, e8, f32 = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float32
+    s = Shape(T, D, H, E, 1, 0, 0, _dt(x), 1)
+    args = (_shaped(W1, e4, (*lead, H, _value_cols(D)), "weights W1"),
+            _shaped(W1_scale, e8, (*lead, -(-H // 128), _scale_cols(D)), "W1_scale"),
+            _shaped_or_none(b1, f32, (*lead, H), "b1"),
+            _shaped(W2, e4, (*lead, D, _value_cols(H)), "weights W2"),
+            _shaped(W2_scale, e8, (*lead, -(-D // 128), _scale_cols(H)), "W2_scale"),
+            _shaped_or_none(b2, f32, (*lead, D), "b2"),
+            _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets"))
+    xp, st = _ptr(x), _queue(x, stream)
     ws = alloc_quantized_workspace(s, x.device) if ws is None else ws
-    y = torch.empty((T, D), dtype=x.dtype, device=x.device) if out is None else out
-    if y.dtype != x.dtype or y.shape != x.shape:
-        raise ClearMoEError("out must have x's shape and dtype")
-    rc = lib().clearmoe_quantized_ffn_forward(
-        ctypes.byref(s), _p(x), _p(W1), _scales(W1_scale, lead + (-(-H // 128), _scale_cols(D)), "W1_scale"), _p(b1),
-        _p(W2), _scales(W2_scale, lead + (-(-D // 128), _scale_cols(H)), "W2_scale"), _p(b2), _p(offsets), _p(y),
-        _p(ws), ws.numel(), _stream(stream))
+    y = torch.empty_like(x) if out is None else out
+    rc = lib().clearmoe_quantized_ffn_forward(ctypes.byref(s), xp, *args, _shaped(y, x.dtype, (T, D), "out"),
+                                              _ptr(ws), ws.numel(), st)
     _check(rc, "clearmoe_quantized_ffn_forward")
     return y
 

@@ -1510,7 +1510,7 @@ namespace {
 struct FewLayout {
     size_t idx, gate, part, route, total;
 };
-constexpr int64_t kFewMaxColumns = 16384;      // r + k q: the second kernel's LDS
+constexpr int64_t kFewMaxColumns = 12288;      // r + k q: the second kernel's LDS
 int check_few(const clearmoe_shape* shape) {
     const int rc = check_shape(shape, true, true);
     if (rc != CLEARMOE_OK) return rc;
@@ -1528,7 +1528,7 @@ FewLayout few_layout(const clearmoe_shape& s) {
     };
     L.idx = take(sizeof(int32_t) * s.T * s.k);
     L.gate = take(sizeof(float) * s.T * s.k);
-    L.part = take(few_part_bytes(s.dtype, s.T, s.H, s.r, s.k, s.q));
+    L.part = take(few_part_bytes(s.T, s.H, s.r, s.k, s.q));
     L.route = off;
     clearmoe_shape rs = s;
     rs.H = rs.r = rs.q = 0;

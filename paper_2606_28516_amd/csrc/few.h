@@ -23,10 +23,10 @@ struct FewArgs {
 
 // Hidden slices (the first kernel's workgroups per token group) and the bytes
 // of the partial sums.
-int few_slices(int dtype, int H);
-size_t few_part_bytes(int dtype, int64_t T, int H, int r, int k, int q);
-// Two kernels; aligned: D, H, r, q and every matrix are whole 16-byte pieces.
-hipError_t launch_few_hidden(int dtype, bool aligned, const FewArgs& a, hipStream_t st);
-hipError_t launch_few_out(int dtype, bool aligned, const FewArgs& a, hipStream_t st);
+int few_slices(int H);
+size_t few_part_bytes(int64_t T, int H, int r, int k, int q);
+// Two kernels; whole: the rows of every matrix are whole, aligned 16-byte pieces.
+hipError_t launch_few_hidden(int dtype, bool whole, const FewArgs& a, hipStream_t st);
+hipError_t launch_few_out(int dtype, bool whole, const FewArgs& a, hipStream_t st);
 
 }  // namespace clearmoe

@@ -1538,8 +1538,13 @@ FewLayout few_layout(const clearmoe_shape& s) {
 }
 
 struct QuantizedLayout {
-    size_t xv, xs, zv, zs, total;
+    size_t xv, xs, zv, zs;     // x and z quantised
+    size_t z;                  // or z in float32, where every workgroup quantises the few rows itself
+    size_t total;
 };
+bool quantized_few(const clearmoe_shape& s) {
+    return q8_few_supported(s.T, q8_cols(s.D)) && q8_few_supported(s.T, q8_cols(s.H));
+}
 QuantizedLayout quantized_layout(const clearmoe_shape& s) {
     QuantizedLayout L{};
     size_t off = 0;
@@ -1548,6 +1553,11 @@ QuantizedLayout quantized_layout(const clearmoe_shape& s) {
         off += up(static_cast<size_t>(s.T) * static_cast<size_t>(bytes) + 1);
         return at;
     };
+    if (quantized_few(s)) {
+        L.z = take(static_cast<int64_t>(sizeof(float)) * s.H);
+        L.total = off;
+        return L;
+    }
     L.xv = take(q8_cols(s.D));
     L.xs = take(q8_scale_cols(s.D));
     L.zv = take(q8_cols(s.H));
@@ -1700,6 +1710,26 @@ int clearmoe_quantized_ffn_forward(const clearmoe_shape* shape, const void* x, c
     const QuantizedLayout L = quantized_layout(s);
     if (!ws || !aligned(ws, kAlign) || ws_bytes < L.total) return CLEARMOE_ERR_WORKSPACE;
     if (s.T == 0) return CLEARMOE_OK;
+    if (quantized_few(s)) {
+        Q8Desc g{};
+        g.M = s.T;
+        g.seg_offsets = offsets; g.nseg = offsets ? s.E : 0;
+        auto product = [&](const void* W, const void* scale, const float* bias, int N, int K, void* c) {
+            g.N = N; g.K = static_cast<int>(q8_cols(K));
+            g.B = static_cast<const uint8_t*>(W); g.b_seg_stride = static_cast<int64_t>(N) * g.K;
+            g.SB = static_cast<const uint8_t*>(scale); g.sb_ld = q8_scale_cols(K);
+            g.sb_seg_stride = q8_blocks(N) * g.sb_ld;
+            g.bias = bias;
+            g.C = c; g.ldc = N;
+        };
+        product(W1, W1_scale, b1, s.H, s.D, at<void>(ws, L.z));
+        g.gelu = 1; g.out = kQ8OutF32;
+        CLEARMOE_STAGE(CLEARMOE_STAGE_FC1, stream, launch_q8_few(g, x, s.dtype == CLEARMOE_F32, s.D, stream));
+        product(W2, W2_scale, b2, s.D, s.H, y);
+        g.gelu = 0; g.out = s.dtype == CLEARMOE_F32 ? kQ8OutF32 : kQ8OutBf16;
+        CLEARMOE_STAGE(CLEARMOE_STAGE_DENSE_FC2, stream, launch_q8_few(g, at<void>(ws, L.z), true, s.H, stream));
+        return CLEARMOE_OK;
+    }
     rc = clearmoe_quantize(s.dtype, CLEARMOE_E4M3, 1, 1, s.T, s.D, x, s.D, at<void>(ws, L.xv), at<void>(ws, L.xs),
                            stream);
     if (rc != CLEARMOE_OK) return rc;

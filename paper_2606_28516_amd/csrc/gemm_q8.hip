@@ -163,6 +163,96 @@ hipError_t q8_rows(const Q8Desc& g, hipStream_t st) {
     return hipGetLastError();
 }
 
+// A few rows of float32 or bfloat16, quantised by every workgroup for itself
+// into LDS (rows of `pitch` bytes, then rows of nk scale bytes), then as
+// k_q8_rows.  The first blocks of B are on their way meanwhile, so a call is
+// two trips to memory at most.
+template <typename TA, typename TC>
+__global__ __launch_bounds__(512) void k_q8_few(Q8Desc g, const TA* A, int K0, int mtiles, int ntiles, int pitch) {
+    constexpr int BM = 16, BN = 16, KW = 8, AHEAD = 4;
+    extern __shared__ __attribute__((aligned(16))) unsigned char s_a[];
+    __shared__ float s_acc[KW][BM][BN + 4];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row = lane & 15, grp = lane >> 4;
+    GbTile t;
+    if (!gb_tile<BM>(g, mtiles, ntiles, 1, lane, t)) return;
+    const int n0 = t.nt * BN, n = n0 + row, nk = static_cast<int>(q8_blocks(g.K));
+    const bool nok = n < g.N, mok = row < t.rows;
+    const uint8_t* br = g.B + t.seg * g.b_seg_stride + static_cast<int64_t>(nok ? n : 0) * g.K;
+    const uint8_t* sb = g.SB + t.seg * g.sb_seg_stride + n0 / kQ8Block * g.sb_ld;
+    i32x8 fb[AHEAD];
+    int kb_scale[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        const int kb = wave + i * KW;
+        fb[i] = q8_frag(br, kb * kQ8Block + grp * 32, g.K, nok);
+        kb_scale[i] = sb[kb < nk ? kb : 0];
+    }
+    // 16 lanes a block of 128 columns
+    unsigned char* s_sa = s_a + t.rows * pitch;
+    for (int u = tid / kQ8Lanes; u < t.rows * nk; u += 512 / kQ8Lanes) {
+        const int m = u / nk, blk = u - m * nk, sub = tid % kQ8Lanes;
+        float f[8];
+        q8_load8(A + (t.m_lo + m) * K0, blk * kQ8Block + sub * 8, K0, f);
+        float a = q8_mag8(f);
+#pragma unroll
+        for (int s = kQ8Lanes / 2; s > 0; s >>= 1) a = fmaxf(a, __shfl_xor(a, s));
+        const int e = q8_exponent(__float_as_uint(a), q8_top_exp(kQ8E4M3));
+        *reinterpret_cast<uint2*>(s_a + m * pitch + blk * kQ8Block + sub * 8) = q8_pack8<kQ8E4M3>(f, q8_two_to(-e));
+        if (sub == 0) s_sa[m * nk + blk] = static_cast<unsigned char>(e + kQ8One);
+    }
+    __syncthreads();
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto step = [&](int kb, const i32x8& b, int scale) {
+        const unsigned char* p = s_a + (mok ? row : 0) * pitch + kb * kQ8Block + grp * 32;
+        i32x8 a;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = mok ? reinterpret_cast<const int*>(p)[i] : 0;
+        const int sa = s_sa[(mok ? row : 0) * nk + kb];
+        if constexpr (sizeof(TC) == 4) {
+            // float32 results: as in k_q8_rows
+            f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q8_widen<kQ8E4M3>(b, i), q8_widen<kQ8E4M3>(a, i), c, 0, 0, 0);
+            const float ka = q8_scale(sa), kb_ = q8_scale(scale);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[v] += c[v] * ka * kb_;
+        } else {
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, kQ8E4M3, kQ8E4M3, 0, scale, 0, sa);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (wave + i * KW < nk) step(wave + i * KW, fb[i], kb_scale[i]);
+    for (int kb = wave + AHEAD * KW; kb < nk; kb += KW)
+        step(kb, q8_frag(br, kb * kQ8Block + grp * 32, g.K, nok), sb[kb]);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) s_acc[wave][row][4 * grp + v] = acc[v];
+    __syncthreads();
+    const int m = tid / BN, c = tid % BN;
+    if (m < t.rows && n0 + c < g.N) {
+        float v = g.bias != nullptr ? g.bias[static_cast<int64_t>(t.seg) * g.N + n0 + c] : 0.0f;
+#pragma unroll
+        for (int w = 0; w < KW; ++w) v += s_acc[w][m][c];
+        if (g.gelu) v = gelu_erf(v);
+        static_cast<TC*>(g.C)[(t.m_lo + m) * g.ldc + n0 + c] = Elem<TC>::from_f32(v);
+    }
+}
+
+template <typename TA, typename TC>
+hipError_t q8_few(const Q8Desc& g, const void* A, int K0, hipStream_t st) {
+    const int64_t mt = (g.M + 15) / 16 + (g.seg_offsets != nullptr ? g.nseg : 0), nt = (g.N + 15) / 16;
+    const int64_t grid = (mt * nt + kGbXcds - 1) / kGbXcds * kGbXcds;
+    const int nk = static_cast<int>(q8_blocks(g.K)), pitch = nk * kQ8Block + 16;
+    const int rows = g.M < 16 ? static_cast<int>(g.M) : 16;
+    launch_kernel(k_q8_few<TA, TC>, dim3(static_cast<unsigned>(grid)), dim3(512),
+                  static_cast<size_t>(rows) * (pitch + nk), st, g, static_cast<const TA*>(A), K0,
+                  static_cast<int>(mt), static_cast<int>(nt), pitch);
+    return hipGetLastError();
+}
+
 // ---------------------------------------------------------------------------
 // Many rows: tiles through LDS.
 // ---------------------------------------------------------------------------
@@ -510,7 +600,21 @@ hipError_t q8_formats(const Q8Desc& g, hipStream_t st) {
     return q8_rows<FA, FB, 8, 2, false>(g, st);
 }
 
+// Rows up to which quantising them in every workgroup pays, and the LDS that
+// their quantised form may take.
+constexpr int64_t kQ8FewRows = 16, kQ8FewLds = 48 << 10;
+
 }  // namespace
+
+bool q8_few_supported(int64_t M, int64_t K) {
+    const int64_t rows = M < 16 ? M : 16;
+    return M <= kQ8FewRows && rows * (q8_blocks(K) * (kQ8Block + 1) + 16) <= kQ8FewLds;
+}
+hipError_t launch_q8_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStream_t st) {
+    if (g.M == 0) return hipSuccess;
+    if (g.out == kQ8OutF32) return a_f32 ? q8_few<float, float>(g, A, K0, st) : q8_few<bf16_bits, float>(g, A, K0, st);
+    return a_f32 ? q8_few<float, bf16_bits>(g, A, K0, st) : q8_few<bf16_bits, bf16_bits>(g, A, K0, st);
+}
 
 hipError_t launch_gemm_q8(const Q8Desc& g, hipStream_t st) {
     if (g.M == 0) return hipSuccess;

@@ -55,6 +55,39 @@ __device__ __forceinline__ uint32_t q8_pack4(float a, float b, float c, float d)
     return static_cast<uint32_t>(v);
 }
 
+// A lane's share of a 128-column block when 16 lanes quantise it: columns
+// [c, c + 8) of a row, zeros from n on.  (A piece may start at any element:
+// the hardware loads it all the same.)
+constexpr int kQ8Lanes = 16;
+template <typename T>
+__device__ __forceinline__ void q8_load8(const T* row, int64_t c, int64_t n, float (&v)[8]) {
+    if (c + 8 > n) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < n ? Elem<T>::load(row, c + i) : 0.0f;
+    } else if constexpr (sizeof(T) == 4) {
+        __builtin_memcpy(v, row + c, 32);
+    } else {
+        u32x4 a;
+        __builtin_memcpy(&a, row + c, 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(a[i] << 16);
+            v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+        }
+    }
+}
+__device__ __forceinline__ float q8_mag8(const float (&v)[8]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, q8_mag(v[i]));
+    return m;
+}
+template <int FMT>
+__device__ __forceinline__ uint2 q8_pack8(const float (&v)[8], float s) {
+    return make_uint2(q8_pack4<FMT>(v[0] * s, v[1] * s, v[2] * s, v[3] * s),
+                      q8_pack4<FMT>(v[4] * s, v[5] * s, v[6] * s, v[7] * s));
+}
+
 // x [batch, rows, cols] (dtype, row stride ldx elements, batches rows * ldx
 // apart) -> v, scale; block_rows 1 or 128.
 hipError_t launch_quantize(int dtype, int fmt, int block_rows, int64_t batch, int64_t rows, int64_t cols,
@@ -84,5 +117,13 @@ struct Q8Desc {
     int seg_merge;               // always 0 (the tile search's field)
 };
 hipError_t launch_gemm_q8(const Q8Desc& g, hipStream_t st);
+
+// The same product in e4m3 for a few rows of A that are still float32
+// (a_f32) or bfloat16 [M, K0] (row stride K0, K = q8_cols(K0)): every workgroup
+// quantises its rows of A itself, in blocks of 128 columns, so that a
+// quantising pass over them is not a launch of its own.  float32 or bfloat16
+// results; SA, A, lda, fa and fb are not used.
+bool q8_few_supported(int64_t M, int64_t K);
+hipError_t launch_q8_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStream_t st);
 
 }  // namespace clearmoe

@@ -9,59 +9,24 @@ namespace clearmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kLanes = 16;               // lanes of a 128-column block, eight columns each
-
-// Columns [c, c + 8) of a row (zeros from n on).  vec: 16-byte loads.
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t n, bool vec, float (&v)[8]) {
-    if (vec && c + 8 <= n) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = *reinterpret_cast<const float4*>(row + c), b = *reinterpret_cast<const float4*>(row + c + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const u32x4 a = *reinterpret_cast<const u32x4*>(row + c);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float(a[i] << 16);
-                v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-            }
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < n ? Elem<T>::load(row, c + i) : 0.0f;
-}
-
-__device__ __forceinline__ float mag8(const float (&v)[8]) {
-    float m = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, q8_mag(v[i]));
-    return m;
-}
-
-template <int FMT>
-__device__ __forceinline__ uint2 pack8(const float (&v)[8], float s) {
-    return make_uint2(q8_pack4<FMT>(v[0] * s, v[1] * s, v[2] * s, v[3] * s),
-                      q8_pack4<FMT>(v[4] * s, v[5] * s, v[6] * s, v[7] * s));
-}
+constexpr int kLanes = kQ8Lanes;
 
 // 1 x 128 blocks: 16 lanes a block.
 template <typename T, int FMT>
 __global__ __launch_bounds__(kThreads) void k_quantize_rows(const T* x, int64_t ldx, int64_t rows, int64_t cols,
-                                                            bool vec, uint8_t* v, uint8_t* scale) {
+                                                            uint8_t* v, uint8_t* scale) {
     const int64_t blocks = q8_blocks(cols), vcols = q8_cols(cols), scols = q8_scale_cols(cols);
     const int sub = threadIdx.x % kLanes;
     const int64_t b = static_cast<int64_t>(blockIdx.x) * (kThreads / kLanes) + threadIdx.x / kLanes;
     if (b >= rows * blocks) return;
     const int64_t row = b / blocks, blk = b - row * blocks, c = blk * kQ8Block + sub * 8;
     float f[8];
-    load8(x + row * ldx, c, cols, vec, f);
-    float m = mag8(f);
+    q8_load8(x + row * ldx, c, cols, f);
+    float m = q8_mag8(f);
 #pragma unroll
     for (int s = kLanes / 2; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
     const int e = q8_exponent(__float_as_uint(m), q8_top_exp(FMT));
-    if (c < vcols) *reinterpret_cast<uint2*>(v + row * vcols + c) = pack8<FMT>(f, q8_two_to(-e));
+    if (c < vcols) *reinterpret_cast<uint2*>(v + row * vcols + c) = q8_pack8<FMT>(f, q8_two_to(-e));
     if (sub == 0) {
         uint8_t* s = scale + row * scols;
         s[blk] = static_cast<uint8_t>(e + kQ8One);
@@ -74,7 +39,7 @@ __global__ __launch_bounds__(kThreads) void k_quantize_rows(const T* x, int64_t 
 // maximum and the rounding.
 template <typename T, int FMT>
 __global__ __launch_bounds__(kThreads) void k_quantize_square(const T* x, int64_t ldx, int64_t rows, int64_t cols,
-                                                              bool vec, uint8_t* v, uint8_t* scale) {
+                                                              uint8_t* v, uint8_t* scale) {
     constexpr int PASS = kThreads / kLanes, NP = kQ8Block / PASS;       // rows a pass, passes
     __shared__ float s_m[kThreads / 64];
     const int64_t blocks = q8_blocks(cols), vcols = q8_cols(cols), scols = q8_scale_cols(cols);
@@ -87,10 +52,10 @@ __global__ __launch_bounds__(kThreads) void k_quantize_square(const T* x, int64_
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         const int64_t row = r0 + p * PASS + rl;
-        load8(xb + (row < rows ? row : 0) * ldx, c, row < rows ? cols : 0, vec, f[p]);
+        q8_load8(xb + (row < rows ? row : 0) * ldx, c, row < rows ? cols : 0, f[p]);
     }
 #pragma unroll
-    for (int p = 0; p < NP; ++p) m = fmaxf(m, mag8(f[p]));
+    for (int p = 0; p < NP; ++p) m = fmaxf(m, q8_mag8(f[p]));
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
     if (threadIdx.x % 64 == 0) s_m[threadIdx.x / 64] = m;
@@ -103,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void k_quantize_square(const T* x, int64_
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         const int64_t row = r0 + p * PASS + rl;
-        if (row < rows && c < vcols) *reinterpret_cast<uint2*>(vb + row * vcols + c) = pack8<FMT>(f[p], k);
+        if (row < rows && c < vcols) *reinterpret_cast<uint2*>(vb + row * vcols + c) = q8_pack8<FMT>(f[p], k);
     }
     if (threadIdx.x == 0) {
         uint8_t* s = scale + br * scols;
@@ -116,16 +81,15 @@ __global__ __launch_bounds__(kThreads) void k_quantize_square(const T* x, int64_
 template <typename T, int FMT>
 hipError_t quantize(int block_rows, int64_t batch, int64_t rows, int64_t cols, const T* x, int64_t ldx, uint8_t* v,
                     uint8_t* scale, hipStream_t st) {
-    const bool vec = ldx % Elem<T>::per16 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
     const int64_t blocks = q8_blocks(cols);
     if (block_rows == 1) {
         const int64_t n = batch * rows * blocks, grid = (n + kThreads / kLanes - 1) / (kThreads / kLanes);
         launch_kernel(k_quantize_rows<T, FMT>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st, x, ldx,
-                      batch * rows, cols, vec, v, scale);
+                      batch * rows, cols, v, scale);
     } else {
         const int64_t grid = batch * ((rows + kQ8Block - 1) / kQ8Block) * blocks;
         launch_kernel(k_quantize_square<T, FMT>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st, x, ldx,
-                      rows, cols, vec, v, scale);
+                      rows, cols, v, scale);
     }
     return hipGetLastError();
 }

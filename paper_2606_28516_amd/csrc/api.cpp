@@ -1657,7 +1657,7 @@ int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, cons
     if (!byte_format(p.a_format) || !byte_format(p.b_format)) return CLEARMOE_ERR_UNSUPPORTED;
     if (!bytes && p.out != CLEARMOE_F32 && p.out != CLEARMOE_BF16) return CLEARMOE_ERR_UNSUPPORTED;
     if (p.M < 0 || p.M >= (int64_t{1} << 31) || p.N < 1 || p.N > kMaxDim || p.K < 16 || p.K > kMaxDim ||
-        p.K % 16 != 0)
+        p.K % 16 != 0 || p.M > (int64_t{1} << 44) / p.N)
         return CLEARMOE_ERR_INVALID_ARG;
     if (p.groups < 0 || p.groups > 64 || (p.gelu != 0 && p.gelu != 1) || p.reserved != 0)
         return CLEARMOE_ERR_INVALID_ARG;

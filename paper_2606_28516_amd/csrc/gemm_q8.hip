@@ -22,8 +22,8 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // ---------------------------------------------------------------------------
-// A few rows: 16 rows x 16 columns (or x 128 for an 8-bit result, whose
-// scales need whole blocks), operands straight from memory into registers.
+// A few rows: 16 rows x 16 columns, operands straight from memory into
+// registers.
 // ---------------------------------------------------------------------------
 // Bytes [k, k + 32) of a row (zeros from K on): lane group g of four takes
 // k = 32 g of a 128-wide block, so four lanes read a whole line of a row.
@@ -67,29 +67,25 @@ __device__ __forceinline__ float q8_scale(uint32_t b) {
     return b == 0 ? 0x1p-127f : b == 255 ? __builtin_nanf("") : __uint_as_float(b << 23);
 }
 
-// CW waves side by side along the columns, KW sharing the sum; WIDE: float32
-// results.
-template <int FA, int FB, int CW, int KW, bool WIDE>
-__global__ __launch_bounds__(64 * CW * KW) void k_q8_rows(Q8Desc g, int mtiles, int ntiles) {
-    constexpr int BM = 16, BN = 16 * CW, PITCH = BN + 4;
-    __shared__ float s_acc[KW][BM][PITCH];
+// Eight waves share the sum.  WIDE: float32 results.
+template <int FA, int FB, bool WIDE>
+__global__ __launch_bounds__(512) void k_q8_rows(Q8Desc g, int mtiles, int ntiles) {
+    constexpr int BM = 16, BN = 16, KW = 8;
+    __shared__ float s_acc[KW][BM][BN + 4];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = lane & 15, grp = lane >> 4;
     GbTile t;
     if (!gb_tile<BM>(g, mtiles, ntiles, 1, lane, t)) return;
-    const int n0 = t.nt * BN, cw = wave % CW, kw = wave / CW;
-    const uint8_t* B = g.B + t.seg * g.b_seg_stride;
-    const int n = n0 + cw * 16 + row;
+    const int n0 = t.nt * BN, n = n0 + row;
     const bool mok = row < t.rows, nok = n < g.N;
     const uint8_t* ar = g.A + (t.m_lo + (mok ? row : 0)) * g.lda;
-    const uint8_t* br = B + static_cast<int64_t>(nok ? n : 0) * g.K;
+    const uint8_t* br = g.B + t.seg * g.b_seg_stride + static_cast<int64_t>(nok ? n : 0) * g.K;
     const uint8_t* sa = g.SA + (t.m_lo + (mok ? row : 0)) * g.sa_ld;
-    // the wave's 16 columns lie in one block
-    const uint8_t* sb = g.SB + t.seg * g.sb_seg_stride + (n0 + cw * 16) / kQ8Block * g.sb_ld;
+    const uint8_t* sb = g.SB + t.seg * g.sb_seg_stride + n0 / kQ8Block * g.sb_ld;     // 16 columns of one block
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     const int nk = static_cast<int>(q8_blocks(g.K));
-    for (int kb = kw; kb < nk; kb += KW) {
+    for (int kb = wave; kb < nk; kb += KW) {
         const i32x8 fa = q8_frag(ar, kb * kQ8Block + grp * 32, g.K, mok);
         const i32x8 fb = q8_frag(br, kb * kQ8Block + grp * 32, g.K, nok);
         if constexpr (WIDE) {
@@ -107,58 +103,25 @@ __global__ __launch_bounds__(64 * CW * KW) void k_q8_rows(Q8Desc g, int mtiles, 
     }
     // result v of a lane: column 4 grp + v of row `row`
 #pragma unroll
-    for (int v = 0; v < 4; ++v) s_acc[kw][row][cw * 16 + 4 * grp + v] = acc[v];
+    for (int v = 0; v < 4; ++v) s_acc[wave][row][4 * grp + v] = acc[v];
     __syncthreads();
-    const float* bias = g.bias == nullptr ? nullptr : g.bias + static_cast<int64_t>(t.seg) * g.N;
-    auto value = [&](int m, int c) {
-        float v = 0.0f;
+    const int m = tid / BN, c = tid % BN;
+    if (m < t.rows && n0 + c < g.N) {
+        float v = g.bias != nullptr ? g.bias[static_cast<int64_t>(t.seg) * g.N + n0 + c] : 0.0f;
 #pragma unroll
         for (int w = 0; w < KW; ++w) v += s_acc[w][m][c];
-        if (n0 + c >= g.N) return 0.0f;
-        if (bias != nullptr) v += bias[n0 + c];
-        return g.gelu ? gelu_erf(v) : v;
-    };
-    if constexpr (CW == 1) {
-        const int m = tid / 16, c = tid % 16;
-        if (m < t.rows && n0 + c < g.N) {
-            const float v = value(m, c);
-            const int64_t at = (t.m_lo + m) * g.ldc + n0 + c;
-            if constexpr (WIDE) static_cast<float*>(g.C)[at] = v;
-            else static_cast<bf16_bits*>(g.C)[at] = f32_to_bf16(v);
-        }
-    } else {
-        static_assert(CW == 8, "a wave finishes a row of one block");
-        const int64_t vcols = q8_cols(g.N), blocks = q8_blocks(g.N);
-        for (int m = wave; m < t.rows; m += CW * KW) {
-            const int c = 2 * lane;
-            const float v0 = value(m, c), v1 = value(m, c + 1);
-            float a = fmaxf(q8_mag(v0), q8_mag(v1));
-#pragma unroll
-            for (int s = 32; s > 0; s >>= 1) a = fmaxf(a, __shfl_xor(a, s));
-            const int fmt = g.out == kQ8OutE4M3 ? kQ8E4M3 : kQ8E5M2;
-            const int e = q8_exponent(__float_as_uint(a), q8_top_exp(fmt));
-            const float k = q8_two_to(-e);
-            const uint32_t p = fmt == kQ8E4M3 ? q8_pack4<kQ8E4M3>(v0 * k, v1 * k, 0.0f, 0.0f)
-                                              : q8_pack4<kQ8E5M2>(v0 * k, v1 * k, 0.0f, 0.0f);
-            if (n0 + c < vcols)
-                *reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(g.C) + (t.m_lo + m) * g.ldc + n0 + c) =
-                    static_cast<uint16_t>(p);
-            if (lane == 0) {
-                uint8_t* s = g.SC + (t.m_lo + m) * g.sc_ld;
-                s[t.nt] = static_cast<uint8_t>(e + kQ8One);
-                if (t.nt == blocks - 1)
-                    for (int64_t i = blocks; i < g.sc_ld; ++i) s[i] = kQ8One;
-            }
-        }
+        if (g.gelu) v = gelu_erf(v);
+        const int64_t at = (t.m_lo + m) * g.ldc + n0 + c;
+        if constexpr (WIDE) static_cast<float*>(g.C)[at] = v;
+        else static_cast<bf16_bits*>(g.C)[at] = f32_to_bf16(v);
     }
 }
 
-template <int FA, int FB, int CW, int KW, bool WIDE>
+template <int FA, int FB, bool WIDE>
 hipError_t q8_rows(const Q8Desc& g, hipStream_t st) {
-    const int64_t mt = (g.M + 15) / 16 + (g.seg_offsets != nullptr ? g.nseg : 0);
-    const int64_t nt = (g.N + 16 * CW - 1) / (16 * CW);
+    const int64_t mt = (g.M + 15) / 16 + (g.seg_offsets != nullptr ? g.nseg : 0), nt = (g.N + 15) / 16;
     const int64_t grid = (mt * nt + kGbXcds - 1) / kGbXcds * kGbXcds;
-    launch_kernel(k_q8_rows<FA, FB, CW, KW, WIDE>, dim3(static_cast<unsigned>(grid)), dim3(64 * CW * KW), 0, st, g,
+    launch_kernel(k_q8_rows<FA, FB, WIDE>, dim3(static_cast<unsigned>(grid)), dim3(512), 0, st, g,
                   static_cast<int>(mt), static_cast<int>(nt));
     return hipGetLastError();
 }
@@ -306,26 +269,33 @@ __device__ __forceinline__ uint32_t q8_pack4_over(float a, float b, float c, flo
     return __builtin_bit_cast(uint32_t, v);
 }
 
-// Sums of a wave's 32 TM rows x 128 columns from c start at the bias, which
-// saves an addition a value at the end; it is put in the lanes' order through
-// 512 bytes of this wave's own LDS.
-template <int TM>
-__device__ __forceinline__ void q8_start(const Q8Desc& g, int seg, int c, int lane, unsigned char* wb,
-                                         f32x16 (&acc)[TM][4]) {
-    if (g.bias == nullptr) {
-        gb_zero(acc);
-        return;
-    }
-    const float* p = g.bias + static_cast<int64_t>(seg) * g.N;
-    const __amdgpu_buffer_rsrc_t rb = raw_rsrc(p, static_cast<int64_t>(g.N) * 4);
-    const int lh = lane >> 5;
+// Sums start at the bias, which saves an addition a value at the end.  Its
+// values for a wave's 32 TN columns from c are put in the lanes' order through
+// 128 TN bytes of the wave's own LDS (wb): here in registers on the way, or
+// fetched by q8_bias_dma and waited for by the caller.
+__device__ __forceinline__ gb_i32x4 q8_bias_desc(const Q8Desc& g, int seg) {
+    return gb_desc(g.bias + static_cast<int64_t>(seg) * g.N, static_cast<int64_t>(g.N) * 4);
+}
+template <int TN>
+__device__ __forceinline__ void q8_bias_dma(const Q8Desc& g, int seg, int c, int lane, uint32_t wb) {
+    const gb_i32x4 d = q8_bias_desc(g, seg);
+    static_assert(TN <= 2, "a word a lane");
+    gb_dma4(d, lane < 32 * TN ? static_cast<uint32_t>(c + lane) * 4u : kGbOob, 0, __builtin_amdgcn_readfirstlane(wb));
+}
+template <int TN>
+__device__ __forceinline__ void q8_bias_load(const Q8Desc& g, int seg, int c, int lane, unsigned char* wb) {
+    const __amdgpu_buffer_rsrc_t rb = raw_rsrc(g.bias + static_cast<int64_t>(seg) * g.N, static_cast<int64_t>(g.N) * 4);
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < TN / 2; ++h)
         reinterpret_cast<float*>(wb)[h * 64 + lane] =
             __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, (c + h * 64 + lane) * 4, 0, 0));
     __builtin_amdgcn_wave_barrier();
+}
+template <int TM, int TN>
+__device__ __forceinline__ void q8_start(int lane, const unsigned char* wb, f32x16 (&acc)[TM][TN]) {
+    const int lh = lane >> 5;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
             const f32x4 b =
@@ -338,26 +308,73 @@ __device__ __forceinline__ void q8_start(const Q8Desc& g, int seg, int c, int la
     __builtin_amdgcn_wave_barrier();
 }
 
-// Epilogue of one wave: 32 TM rows from rw, the 128 columns of scale block
-// blk.  Lane l holds row i * 32 + l % 32 and, for each half h of a tile's 16
-// values, eight consecutive columns (gb_col_of_slot).  Rows are rounded, put
-// together in 32 rows of this wave's own LDS and stored as whole row pieces.
-template <int TM, int OUT>
-__device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, int rw, int blk, int lane,
-                                            unsigned char* wb, bool nt, f32x16 (&acc)[TM][4]) {
-    constexpr int RB = OUT == kQ8OutBf16 ? 256 : 128, CH = RB / 16, RPI = 64 / CH;
-    const int lrow = lane & 31, lh = lane >> 5, nw = blk * kQ8Block;
+// Epilogue of one wave: 32 TM rows from rw, 32 TN columns from nw.  Lane l
+// holds row i * 32 + l % 32 and, for each half h of a tile's 16 values, eight
+// consecutive columns (gb_col_of_slot).  Rows are rounded, put together in 32
+// rows of this wave's own LDS (wb) and stored as whole row pieces.  For an
+// 8-bit result, 128 / (32 TN) waves side by side share a block: they exchange
+// the rows' maxima through s_max [waves side by side][BM], between barriers
+// that all waves of the workgroup take.
+template <int TM, int TN, int OUT, int BM>
+__device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, int rw, int nw, int wn, int lane,
+                                            unsigned char* wb, float* s_max, bool nt, f32x16 (&acc)[TM][TN]) {
+    constexpr bool F32 = OUT == kQ8OutF32, BF16 = OUT == kQ8OutBf16;
+    constexpr int FMT = OUT == kQ8OutE4M3 ? kQ8E4M3 : kQ8E5M2;
+    constexpr int RB = TN * 32 * (F32 ? 4 : BF16 ? 2 : 1), CH = RB / 16, RPI = 64 / CH, SHARE = 4 / TN;
+    static_assert(RB >= 32 && 64 % CH == 0 && 32 % RPI == 0, "whole rows per store");
+    const int lrow = lane & 31, lh = lane >> 5;
     const int cols = static_cast<int>(q8_cols(g.N));
+    if (g.gelu)
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = F32 ? gelu_erf(acc[i][j][v]) : q8_gelu(acc[i][j][v]);
+    float mx[TM];
+    if constexpr (!F32 && !BF16) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            // a lane and the one 32 further hold a row's columns; infinities
+            // (rare: the whole wave looks again) do not set the scale
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) m = fmaxf(m, fabsf(acc[i][j][v]));
+            if (__ballot(!(m < __builtin_inff())) != 0) {
+                m = 0.0f;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) m = fmaxf(m, q8_mag(acc[i][j][v]));
+            }
+            mx[i] = fmaxf(m, __shfl_xor(m, 32));
+            if (SHARE > 1 && lh == 0) s_max[wn * BM + rw + i * 32 + lrow] = mx[i];
+        }
+        if constexpr (SHARE > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int w = 0; w < SHARE; ++w)
+                    mx[i] = fmaxf(mx[i], s_max[(wn / SHARE * SHARE + w) * BM + rw + i * 32 + lrow]);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        if (g.gelu)
+        if constexpr (F32) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][j][v] = q8_gelu(acc[i][j][v]);
-        if constexpr (OUT == kQ8OutBf16) {
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 w = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    const int ch = j * 8 + 4 * (q >> 1) + 2 * lh + (q & 1);
+                    *reinterpret_cast<f32x4*>(wb + lrow * RB + ((ch ^ (lrow % CH)) << 4)) = w;
+                }
+        } else if constexpr (BF16) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     u32x4 w;
@@ -368,33 +385,18 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
                     *reinterpret_cast<u32x4*>(wb + lrow * RB + ((ch ^ (lrow % CH)) << 4)) = w;
                 }
         } else {
-            constexpr int FMT = OUT == kQ8OutE4M3 ? kQ8E4M3 : kQ8E5M2;
-            // a lane and the one 32 further hold a row's block; infinities
-            // (rare: the whole wave looks again) do not set the scale
-            float m = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) m = fmaxf(m, fabsf(acc[i][j][v]));
-            if (__ballot(!(m < __builtin_inff())) != 0) {
-                m = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) m = fmaxf(m, q8_mag(acc[i][j][v]));
-            }
-            m = fmaxf(m, __shfl_xor(m, 32));
-            const int e = q8_exponent(__float_as_uint(m), q8_top_exp(FMT));
+            const int e = q8_exponent(__float_as_uint(mx[i]), q8_top_exp(FMT));
             const float k = q8_two_to(e);
             const int rl = rw + i * 32 + lrow;
-            if (lh == 0 && rl < t.rows) {
+            if (lh == 0 && rl < t.rows && nw % kQ8Block == 0 && nw < g.N) {
                 uint8_t* s = g.SC + (t.m_lo + rl) * g.sc_ld;
+                const int blk = nw / kQ8Block;
                 s[blk] = static_cast<uint8_t>(e + kQ8One);
                 if (nw + kQ8Block >= g.N)                       // the last block fills the row up
                     for (int64_t p = blk + 1; p < g.sc_ld; ++p) s[p] = kQ8One;
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     u32x2 w;
@@ -417,7 +419,17 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
             const u32x4 w = *reinterpret_cast<const u32x4*>(wb + rr * RB + ((ch ^ (rr % CH)) << 4));
             const int rl = rw + i * 32 + rr;
             if (rl >= t.rows) continue;
-            if constexpr (OUT == kQ8OutBf16) {
+            if constexpr (F32) {
+                const int n = nw + ch * 4;
+                float* c = static_cast<float*>(g.C) + (t.m_lo + rl) * g.ldc + n;
+                if (g.wide) {
+                    if (n < g.N) gb_store(reinterpret_cast<u32x4*>(c), w, nt);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (n + q < g.N) c[q] = __uint_as_float(w[q]);
+                }
+            } else if constexpr (BF16) {
                 const int n = nw + ch * 8;
                 bf16_bits* c = static_cast<bf16_bits*>(g.C) + (t.m_lo + rl) * g.ldc + n;
                 if (g.wide) {
@@ -511,7 +523,12 @@ void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
     dma_b(0);
     f32x16 acc[TM][TN];
     // (through the second buffer of A, which is filled after the first wait)
-    q8_start<TM>(g, t.seg, n0, lane, smem + ABUF + wave * 512, acc);
+    if (g.bias != nullptr) {
+        q8_bias_load<TN>(g, t.seg, n0, lane, smem + ABUF + wave * 512);
+        q8_start(lane, smem + ABUF + wave * 512, acc);
+    } else {
+        gb_zero(acc);
+    }
 
     const int bcol = gb_col_of_slot(lrow);
     uint32_t oa[2], ob[2];
@@ -572,7 +589,184 @@ void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
         }
     }
     gb_wait_barrier<0>();                        // the stage buffers are free
-    q8_epilogue<TM, OUT>(g, t, wave * 64, t.nt, lane, smem + wave * (32 * 256), nt_store != 0, acc);
+    q8_epilogue<TM, TN, OUT, BM>(g, t, wave * 64, n0, 0, lane, smem + wave * (32 * 256), nullptr, nt_store != 0, acc);
+}
+
+// WM x WN waves of TM x TN MFMA tiles (32 x 32), NS stages in LDS: of each
+// stage the loads are issued NS - 1 stages ahead, so that the k loop runs at
+// the speed of its loads also where a CU has one workgroup and few of them.
+// Every stage's loads end with the scale words of its rows and columns.
+// WIDE: float32 results, on bfloat16 instructions (see above).
+template <int WM, int WN, int TM, int TN, int NS, int FA, int FB, int OUT>
+__global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
+    constexpr bool WIDE = OUT == kQ8OutF32;
+    constexpr int NW = WM * WN, SB = kGbRow, BM = WM * TM * 32, BN = WN * TN * 32, CPR = 8, BK = kQ8Block;
+    constexpr int AL = BM / (8 * NW), BL = BN / (8 * NW), LPS = AL + BL + 1;
+    static_assert(AL >= 1 && BL >= 1 && BM % 64 == 0 && BN % 64 == 0 && BM + BN <= 64 * NW, "whole loads per wave");
+    static_assert(NS % 2 == 0 && LPS * (NS - 1) < 64, "pipeline");
+    static_assert(kQ8Block % (TN * 32) == 0 && (OUT == kQ8OutF32 || OUT == kQ8OutBf16 || BN % kQ8Block == 0),
+                  "a wave's columns lie in one block, an 8-bit tile has whole blocks");
+    constexpr int STAGE_A = BM * SB, STAGE = (BM + BN) * SB, SOFF = NS * STAGE, SSTAGE = 256 * NW;
+    constexpr int EPI = NW * 32 * TN * 32 * (OUT == kQ8OutF32 ? 4 : OUT == kQ8OutBf16 ? 2 : 1);
+    constexpr int SSIZE = NS * SSTAGE > WN * BM * 4 ? NS * SSTAGE : WN * BM * 4;
+    static_assert(SOFF >= EPI, "the epilogue's rows fit the stages");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[SOFF + SSIZE + NW * 256];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int lrow = lane & 31, lh = lane >> 5, K = g.K;
+
+    GbTile t;
+    if (!gb_tile<BM>(g, mtiles, ntiles, group, lane, t)) return;
+    const int n0 = t.nt * BN;
+    const int nk = static_cast<int>(q8_blocks(K)), left = K - (nk - 1) * BK;
+    const int lr = lane / CPR;
+    // first k of the lane's chunk in an even load's 8 rows; odd: ^ 64
+    const int kc0 = 16 * ((lane % CPR) ^ (lr >> 1));
+    const uint32_t lda = static_cast<uint32_t>(g.lda);
+    const int nrows = g.N - n0 < BN ? g.N - n0 : BN;
+    const gb_i32x4 da = gb_desc(g.A + t.m_lo * g.lda, (static_cast<int64_t>(t.rows) - 1) * g.lda + K);
+    const gb_i32x4 db = gb_desc(g.B + t.seg * g.b_seg_stride + static_cast<int64_t>(n0) * K,
+                                static_cast<int64_t>(nrows) * K);
+    // scale words: the first BM / 64 waves fetch those of the rows, the next
+    // BN / 64 those of the columns (each its block's)
+    const int sr = wave * 64 + lane;
+    const bool s_row = wave < BM / 64;
+    const gb_i32x4 ds = s_row ? gb_desc(g.SA + t.m_lo * g.sa_ld, static_cast<int64_t>(t.rows) * g.sa_ld)
+                              : gb_desc(g.SB + t.seg * g.sb_seg_stride, q8_blocks(g.N) * g.sb_ld);
+    const uint32_t vs = s_row ? (sr < t.rows ? static_cast<uint32_t>(sr) * static_cast<uint32_t>(g.sa_ld) : kGbOob)
+                              : (sr - BM < BN ? static_cast<uint32_t>((n0 + sr - BM) / kQ8Block) *
+                                                    static_cast<uint32_t>(g.sb_ld)
+                                              : kGbOob);
+    // Load i of a wave brings the rows 8 i + lr from its first one on.  Row r
+    // of LDS has its chunk c at c ^ (r / 2 % 8), which for the rows of a load
+    // depends on whether it is an even or odd one of the tile.
+    constexpr int PA = AL > 1 ? 2 : 1, PB = BL > 1 ? 2 : 1;
+    const int oddA = AL == 1 ? wave & 1 : 0, oddB = BL == 1 ? wave & 1 : 0;
+    uint32_t va[PA], vb[PB];
+    int ka[PA], kb[PB];
+#pragma unroll
+    for (int p = 0; p < PA; ++p) {
+        ka[p] = kc0 ^ (64 * ((p + oddA) & 1));
+        va[p] = static_cast<uint32_t>(wave * AL * 8 + lr) * lda + static_cast<uint32_t>(ka[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < PB; ++p) {
+        kb[p] = kc0 ^ (64 * ((p + oddB) & 1));
+        vb[p] = static_cast<uint32_t>((wave * BL * 8 + lr) * K + kb[p]);
+    }
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(
+        static_cast<uint32_t>(reinterpret_cast<uintptr_t>((gb_lds_u32*)smem)));
+    // Stages past the last are issued too (zeros, no memory traffic), so that
+    // every wait below counts the same.  Rows past the tile's lie past the
+    // descriptor's end.
+    auto dma = [&](int kt, int b) {
+        const bool past = kt >= nk;
+        const int soff = __builtin_amdgcn_readfirstlane(past ? 0 : kt * BK);
+#pragma unroll
+        for (int i = 0; i < AL; ++i) {
+            const int p = i % PA;
+            const uint32_t v = past || (kt == nk - 1 && ka[p] >= left) ? kGbOob : va[p];
+            gb_dma16(da, v + static_cast<uint32_t>(8 * i) * lda, soff,
+                     __builtin_amdgcn_readfirstlane(lds0 + b * STAGE + (wave * AL + i) * 1024));
+        }
+#pragma unroll
+        for (int i = 0; i < BL; ++i) {
+            const int p = i % PB;
+            const uint32_t v = past || (kt == nk - 1 && kb[p] >= left) ? kGbOob : vb[p];
+            gb_dma16(db, v + static_cast<uint32_t>(8 * i * K), soff,
+                     __builtin_amdgcn_readfirstlane(lds0 + b * STAGE + STAGE_A + (wave * BL + i) * 1024));
+        }
+        gb_dma4(ds, past ? kGbOob : vs, __builtin_amdgcn_readfirstlane(past ? 0 : (kt & ~3)),
+                __builtin_amdgcn_readfirstlane(lds0 + SOFF + b * SSTAGE + wave * 256));
+    };
+    // (a word a lane whatever TN is: 256 bytes)
+    constexpr int BOFF = SOFF + SSIZE;
+    if (g.bias != nullptr) q8_bias_dma<TN>(g, t.seg, n0 + wn * TN * 32, lane, lds0 + BOFF + wave * 256);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) dma(s, s);
+
+    const int bcol = gb_col_of_slot(lrow);
+    uint32_t oa[2], ob[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        oa[s] = static_cast<uint32_t>((wm * TM * 32 + lrow) * SB + (((4 * s + 2 * lh) ^ gb_swz<SB>(lrow)) << 4));
+        ob[s] = static_cast<uint32_t>(STAGE_A + (wn * TN * 32 + bcol) * SB +
+                                      (((4 * s + 2 * lh) ^ gb_swz<SB>(bcol)) << 4));
+    }
+    i32x8 fa[2][TM], fb[2][TN];
+    uint32_t sa[2][TM], sb[2];                   // by the stage's parity
+    auto read = [&](int b, int s) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[s][j] = q8_lds_frag(smem + b * STAGE + j * 32 * SB, ob[s]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[s][i] = q8_lds_frag(smem + b * STAGE + i * 32 * SB, oa[s]);
+    };
+    auto read_scales = [&](int kt, int b) {
+        const int sh = 8 * (kt & 3);
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(smem + SOFF + b * SSTAGE);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) sa[b & 1][i] = p[wm * TM * 32 + i * 32 + lrow] >> sh;
+        sb[b & 1] = p[BM + wn * TN * 32] >> sh;   // one block
+    };
+    gb_wait_barrier<(NS - 1) * LPS>();           // the bias and stage 0 have landed
+    f32x16 acc[TM][TN];
+    if (g.bias != nullptr) q8_start(lane, smem + BOFF + wave * 256, acc);
+    else gb_zero(acc);
+    read(0, 0);
+    read_scales(0, 0);
+    f32x16 part[WIDE ? TM : 1][WIDE ? TN : 1];
+    for (int k0 = 0; k0 < nk; k0 += NS) {
+#pragma unroll
+        for (int b = 0; b < NS; ++b) {
+            const int kt = k0 + b;
+            if (kt >= nk) break;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (s == 0) {
+                    read(b, 1);
+                } else if (kt + 1 < nk) {
+                    // stage kt + 1 has landed for every wave, and every wave
+                    // is done reading stage kt's buffer, which takes kt + NS
+                    gb_wait_barrier<(NS - 2) * LPS>();
+                    read((b + 1) % NS, 0);
+                    read_scales(kt + 1, (b + 1) % NS);
+                    dma(kt + NS, b);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) {
+                        if constexpr (WIDE) {
+                            f32x16& c = part[i][j];
+                            if (s == 0)
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) c[v] = 0.0f;
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q8_widen<FB>(fb[s][j], q),
+                                                                            q8_widen<FA>(fa[s][i], q), c, 0, 0, 0);
+                            if (s == 1) {
+                                // a lane's results are of the row that its A fragment has
+                                const float fa_ = q8_scale(sa[b & 1][i] & 255u), fb_ = q8_scale(sb[b & 1] & 255u);
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) acc[i][j][v] += c[v] * fa_ * fb_;
+                            }
+                        } else {
+                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                                fb[s][j], fa[s][i], acc[i][j], FB, FA, 0, static_cast<int>(sb[b & 1]), 0,
+                                static_cast<int>(sa[b & 1][i]));
+                        }
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    gb_wait_barrier<0>();                        // the stage buffers are free
+    q8_epilogue<TM, TN, OUT, BM>(g, t, wm * TM * 32, n0 + wn * TN * 32, wn, lane, smem + wave * (EPI / NW),
+                                 reinterpret_cast<float*>(smem + SOFF), nt_store != 0, acc);
 }
 
 // Results of 16 MB or more are written past the L2.
@@ -589,15 +783,54 @@ hipError_t q8_duo(const Q8Desc& g, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <int WM, int WN, int TM, int TN, int NS, int FA, int FB, int OUT>
+hipError_t q8_tile(const Q8Desc& g, hipStream_t st) {
+    constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
+    const int64_t mt = (g.M + BM - 1) / BM + (g.seg_offsets != nullptr ? g.nseg : 0), nt = (g.N + BN - 1) / BN;
+    const int64_t grid = (mt * nt + kGbXcds - 1) / kGbXcds * kGbXcds;
+    const int64_t bytes = g.M * g.N * (OUT == kQ8OutF32 ? 4 : OUT == kQ8OutBf16 ? 2 : 1);
+    launch_kernel(k_q8_tile<WM, WN, TM, TN, NS, FA, FB, OUT>, dim3(static_cast<unsigned>(grid)), dim3(64 * WM * WN), 0,
+                  st, g, static_cast<int>(mt), static_cast<int>(nt), 4, bytes >= kQ8StreamBytes ? 1 : 0);
+    return hipGetLastError();
+}
+
+// Tiles of bm x bn of a product; a group ends inside a tile: half a tile more.
+int64_t q8_tiles(const Q8Desc& g, int bm, int bn) {
+    const int64_t groups = g.seg_offsets != nullptr ? g.nseg : 0;
+    return ((g.M + bm - 1) / bm + groups / 2) * ((g.N + bn - 1) / bn);
+}
+
+// Which kernel: by the number of tiles, that is by how well each fills the
+// chip.  Times in us on an MI355X, N x K of 768 x 3072 and 384 x 1536 to
+// bfloat16 and float32, 3072 x 768 and 1536 x 384 with GELU to 8 bits:
+//                    rows of A   128        1024         4096         16384
+//   bfloat16  16 x 16 (rows)   8.6  4.7  38.0  11.8   141   39
+//             64 x 64          9.2  6.4  10.1   6.7    22.1  8.9     80   24
+//             128 x 128       15.6  9.7  16.5  10.1    19.1 10.8     56   22
+//             256 x 128 (duo) 28.3 16.3  29.4  16.7    32.9 17.3     42   21
+//   float32   16 x 16          9.3        39.4        143
+//             64 x 64         17.6        18.7         39.2         136
+//             128 x 128       32.5        33.5         36.9         108
+//   8 bits    64 x 128         7.2  6.0   9.6   6.2    25.1 11.9     89   35
+//             256 x 128 (duo) 12.8  9.6  13.4  10.0    20.5 11.0     57   25
 template <int FA, int FB>
 hipError_t q8_formats(const Q8Desc& g, hipStream_t st) {
-    if (g.out == kQ8OutF32) return q8_rows<FA, FB, 1, 8, true>(g, st);
-    if (g.M > 64) {
-        if (g.out == kQ8OutBf16) return q8_duo<FA, FB, kQ8OutBf16>(g, st);
-        return g.out == kQ8OutE4M3 ? q8_duo<FA, FB, kQ8OutE4M3>(g, st) : q8_duo<FA, FB, kQ8OutE5M2>(g, st);
+    if (g.out == kQ8OutE4M3 || g.out == kQ8OutE5M2) {
+        // two workgroups of 64 x 128 on every CU, or more rows a workgroup
+        const bool few = q8_tiles(g, 64, 128) <= 512;
+        if (g.out == kQ8OutE4M3)
+            return few ? q8_tile<2, 2, 1, 2, 2, FA, FB, kQ8OutE4M3>(g, st) : q8_duo<FA, FB, kQ8OutE4M3>(g, st);
+        return few ? q8_tile<2, 2, 1, 2, 2, FA, FB, kQ8OutE5M2>(g, st) : q8_duo<FA, FB, kQ8OutE5M2>(g, st);
     }
-    if (g.out == kQ8OutBf16) return q8_rows<FA, FB, 1, 8, false>(g, st);
-    return q8_rows<FA, FB, 8, 2, false>(g, st);
+    if (g.out == kQ8OutF32) {
+        if (q8_tiles(g, 16, 16) <= 800) return q8_rows<FA, FB, true>(g, st);
+        if (q8_tiles(g, 64, 64) <= 1024) return q8_tile<2, 2, 1, 1, 4, FA, FB, kQ8OutF32>(g, st);
+        return q8_tile<4, 2, 1, 2, 4, FA, FB, kQ8OutF32>(g, st);
+    }
+    if (q8_tiles(g, 16, 16) <= 400) return q8_rows<FA, FB, false>(g, st);
+    if (q8_tiles(g, 64, 64) <= 640) return q8_tile<2, 2, 1, 1, 4, FA, FB, kQ8OutBf16>(g, st);
+    if (q8_tiles(g, 256, 128) < 192) return q8_tile<4, 2, 1, 2, 4, FA, FB, kQ8OutBf16>(g, st);
+    return q8_duo<FA, FB, kQ8OutBf16>(g, st);
 }
 
 // Rows up to which quantising them in every workgroup pays, and the LDS that

@@ -37,6 +37,14 @@ __device__ __forceinline__ void gb_dma16(const gb_i32x4& d, uint32_t voff, uint3
                  : "memory", "m0");
 }
 
+// 4 bytes per lane, buffer -> LDS at m0 + 4 * lane.
+__device__ __forceinline__ void gb_dma4(const gb_i32x4& d, uint32_t voff, uint32_t soff, uint32_t m0) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+                 :
+                 : "s"(m0), "v"(voff), "s"(d), "s"(soff)
+                 : "memory", "m0");
+}
+
 // Store of a finished row piece; nt: a streaming store past the L2.
 __device__ __forceinline__ void gb_store(u32x4* p, const u32x4& v, bool nt) {
     if (nt) __builtin_nontemporal_store(v, p);

@@ -208,7 +208,7 @@ def _check_product(M, N, K, E=0, offsets=None, fa=E4M3, fb=E4M3, out=torch.bfloa
 SIZES = [
     (1, 1, 16), (1, 16, 128), (1, 1536, 384), (2, 17, 144), (16, 128, 112), (17, 130, 400), (33, 200, 1040),
     (100, 384, 1536), (129, 257, 272), (300, 1550, 400), (256, 256, 128), (257, 300, 640), (1003, 520, 1200),
-    (512, 512, 2064), (2000, 72, 784), (700, 1032, 128),
+    (512, 512, 2064), (2000, 72, 784), (700, 1032, 128), (4100, 1550, 208), (3000, 1300, 144), (8200, 776, 336),
 ]
 
 
@@ -219,7 +219,7 @@ def test_product(M, N, K, out):
 
 
 @pytest.mark.parametrize("out", [torch.bfloat16, E4M3])
-@pytest.mark.parametrize("M,N,K", [(5, 40, 144), (300, 300, 400)])
+@pytest.mark.parametrize("M,N,K", [(5, 40, 144), (300, 300, 400), (700, 300, 400), (3000, 1300, 144), (4200, 1550, 144)])
 @pytest.mark.parametrize("fa", FMTS)
 @pytest.mark.parametrize("fb", FMTS)
 def test_product_formats(fa, fb, M, N, K, out):
@@ -231,6 +231,7 @@ GROUPS = [
     (900, 130, 272, [0, 1, 300, 300, 557, 813, 900]), (900, 264, 144, [100, 400, 656, 880]),
     (1200, 384, 400, [0, 37, 150, 300, 600, 601, 890, 1100, 1200]),
     (64, 32, 48, list(range(65))), (5, 24, 32, [0, 0, 0, 0]),
+    (4000, 700, 144, [0, 1000, 1001, 2500, 4000]), (6000, 1160, 144, [0, 5, 5, 1700, 3333, 6000]), (7000, 900, 272, [64, 100, 3000, 6900]),
 ]
 
 
@@ -363,7 +364,7 @@ def _ffn_reference(x, w1, b1, w2, b2, D, H, half):
 FLIPS = 2.0 ** -3 * math.sqrt(2 * CUT / 2.0 ** -4)
 
 FFN = [(1, 8, 8), (1, 768, 1536), (3, 100, 390), (16, 384, 1536), (17, 130, 516), (40, 390, 1550), (300, 192, 768),
-       (515, 256, 1030), (1000, 384, 512)]
+       (515, 256, 1030), (1000, 384, 512), (2500, 144, 2000)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])

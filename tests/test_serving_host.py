@@ -106,7 +106,7 @@ def _product(a=A, sa=A, b=A, sb=A, bias=None, offsets=None, c=A, sc=None, **kw):
 
 
 def test_product_refusals():
-    for kw in (dict(M=-1), dict(M=1 << 31), dict(N=0), dict(N=65537), dict(K=0), dict(K=8), dict(K=72), dict(K=65552),
+    for kw in (dict(M=-1), dict(M=1 << 31), dict(M=(1 << 28) + 1, N=65536), dict(N=0), dict(N=65537), dict(K=0), dict(K=8), dict(K=72), dict(K=65552),
                dict(groups=-1), dict(groups=65), dict(gelu=2), dict(reserved=1), dict(lda=48), dict(lda=72),
                dict(lda=(1 << 22) + 16), dict(ldc=39), dict(ldc=(1 << 22) + 1)):
         extra = dict(offsets=A) if kw.get("groups", 0) > 0 else {}

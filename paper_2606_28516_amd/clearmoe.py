@@ -208,7 +208,7 @@ def _queue(x: torch.Tensor, stream) -> int:
     kernels are launched there.  The current stream is asked for by its handle
     (a torch.cuda.Stream object costs 3 us, a quarter of a small call)."""
     dev = x.get_device()
-    if dev != torch.cuda.current_device():
+    if dev != torch._C._cuda_getDevice():
         raise ClearMoEError("the tensors are not on the current device")
     if stream is not None:
         return stream.cuda_stream
@@ -523,8 +523,8 @@ def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
     st = _queue(x, stream)
     dt, code = _dt(x), _format(fmt)
     nr = rows if block_rows == 1 else -(-rows // 128)
-    v = torch.empty((*lead, rows, _value_cols(cols)), dtype=fmt, device=x.device)
-    s = torch.empty((*lead, nr, _scale_cols(cols)), dtype=torch.float8_e8m0fnu, device=x.device)
+    v = x.new_empty((*lead, rows, _value_cols(cols)), dtype=fmt)
+    s = x.new_empty((*lead, nr, _scale_cols(cols)), dtype=torch.float8_e8m0fnu)
     rc = lib().clearmoe_quantize(dt, code, block_rows, batch, rows, cols, x.data_ptr(), ldx, v.data_ptr(),
                                  s.data_ptr(), st)
     _check(rc, "clearmoe_quantize")
@@ -554,8 +554,8 @@ def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offset
             _shaped_or_none(bias, torch.float32, (*lead, N), "bias"),
             _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets"))
     st = _queue(a, stream)
-    c = torch.empty((M, cols), dtype=out_dtype, device=a.device) if out is None else out
-    cs = torch.empty((M, _scale_cols(N)), dtype=e8, device=a.device) if byte else None
+    c = a.new_empty((M, cols), dtype=out_dtype) if out is None else out
+    cs = a.new_empty((M, _scale_cols(N)), dtype=e8) if byte else None
     rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), *args, _shaped(c, out_dtype, (M, cols), "out"), _ptr(cs), st)
     _check(rc, "clearmoe_quantized_gemm")
     return (c, cs) if byte else c

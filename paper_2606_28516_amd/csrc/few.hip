@@ -52,17 +52,20 @@ __device__ __forceinline__ float few_elem(const u32x4& v, int i, bf16_bits) {
     return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
 }
 
-// Row elements [c, c + per16), zeros from column n on or with ok false.  VEC:
-// rows are whole 16-byte pieces; else a piece may start at any element (the
-// hardware loads it all the same) and the row's last, cut one is read element
-// by element.
-template <typename T, bool VEC>
+// How rows are read: whole 16-byte pieces; pieces that may start at any
+// element (the hardware loads them all the same); or, for rows shorter than a
+// piece, element by element.
+enum { kFewWhole, kFewPieces, kFewElems };
+
+// Row elements [c, c + per16), zeros from column n on or with ok false.  The
+// row's last, cut piece is read element by element.
+template <typename T, int MODE>
 __device__ __forceinline__ u32x4 few_load(const T* row, int64_t c, int64_t n, bool ok) {
     constexpr int PER16 = Elem<T>::per16;
     u32x4 v = {0u, 0u, 0u, 0u};
-    if constexpr (VEC) {
+    if constexpr (MODE == kFewWhole) {
         if (ok && c < n) v = *reinterpret_cast<const u32x4*>(row + c);
-    } else if (ok && c + PER16 <= n) {
+    } else if (MODE == kFewPieces && ok && c + PER16 <= n) {
         __builtin_memcpy(&v, row + c, 16);
     } else if (ok && c < n) {
 #pragma unroll
@@ -74,20 +77,39 @@ __device__ __forceinline__ u32x4 few_load(const T* row, int64_t c, int64_t n, bo
     }
     return v;
 }
+// The same for an operand whose partner is read in the same way, so that only
+// the pairs of elements count: a cut last piece is the row's last whole one
+// without the elements that came before.  (No branch: a load that some lanes
+// take apart costs more than the rest of a step.)
+template <typename T, int MODE>
+__device__ __forceinline__ u32x4 few_pair(const T* row, int64_t c, int64_t n, bool ok) {
+    constexpr int PER16 = Elem<T>::per16;
+    if constexpr (MODE != kFewPieces) return few_load<T, MODE>(row, c, n, ok);
+    u32x4 v = {0u, 0u, 0u, 0u};
+    const int64_t at = c + PER16 <= n ? c : n - PER16;
+    if (ok && c < n) __builtin_memcpy(&v, row + at, 16);
+    const int skip = static_cast<int>(c - at);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if constexpr (sizeof(T) == 4) v[w] = w >= skip ? v[w] : 0u;
+        else v[w] = 2 * w >= skip ? v[w] : 2 * w + 1 >= skip ? v[w] & 0xffff0000u : 0u;
+    }
+    return v;
+}
 
 // |v| of each element of a piece.
 __device__ __forceinline__ u32x4 few_abs(u32x4 v, float) { return v & 0x7fffffffu; }
 __device__ __forceinline__ u32x4 few_abs(u32x4 v, bf16_bits) { return v & 0x7fff7fffu; }
 
 // Logits of one token in double into lg[0 .. E) (LDS): an expert a wave.
-template <typename T, bool VEC>
+template <typename T, int MODE>
 __device__ __forceinline__ void few_logits(const FewArgs& a, const T* x, int wave, int lane, double* lg) {
     constexpr int PER16 = Elem<T>::per16;
     for (int e = wave; e < a.E; e += kFewWaves) {
         const T* w = static_cast<const T*>(a.Wg) + static_cast<int64_t>(e) * a.D;
         double s = 0.0;
         for (int64_t c = lane * PER16; c < a.D; c += 64 * PER16) {
-            const u32x4 xv = few_load<T, VEC>(x, c, a.D, true), wv = few_load<T, VEC>(w, c, a.D, true);
+            const u32x4 xv = few_pair<T, MODE>(x, c, a.D, true), wv = few_pair<T, MODE>(w, c, a.D, true);
 #pragma unroll
             for (int i = 0; i < PER16; ++i)
                 s += static_cast<double>(few_elem(xv, i, T{})) * static_cast<double>(few_elem(wv, i, T{}));
@@ -113,10 +135,10 @@ __device__ __forceinline__ int few_rank(const F* lg, int E, int e) {
 
 // Routing of token t for the caller and the second kernel: choice and gates by
 // the rule of the routers, all in double.
-template <typename T, bool VEC>
+template <typename T, int MODE>
 __device__ __forceinline__ void few_route(const FewArgs& a, int t, double* lg, double* ex, int32_t* idx) {
     const int tid = threadIdx.x, E = a.E, k = a.k;
-    few_logits<T, VEC>(a, static_cast<const T*>(a.x) + static_cast<int64_t>(t) * a.D, tid >> 6, tid & 63, lg);
+    few_logits<T, MODE>(a, static_cast<const T*>(a.x) + static_cast<int64_t>(t) * a.D, tid >> 6, tid & 63, lg);
     __syncthreads();
     if (tid < E) {
         const int rank = few_rank(lg, E, tid);
@@ -142,13 +164,13 @@ __device__ __forceinline__ void few_route(const FewArgs& a, int t, double* lg, d
 // Workgroup (slice, token group): z of HS hidden units for up to 16 tokens,
 // then its share of t and the u_j.  The first `routes` workgroups of a group
 // route a token each instead.  EG: 16-expert groups.
-template <typename T, bool VEC, int EG, int HS>
+template <typename T, int MODE, int EG, int HS>
 __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int routes) {
     constexpr int STEP = FewMfma<T>::step, PER16 = Elem<T>::per16;
     constexpr int HT = HS / 16, KW = kFewWaves / HT;          // row tiles of the slice, waves along D
     static_assert((HT == 2 || HT == 4) && kFewGroup * HS % kFewThreads == 0, "waves and values of z");
     constexpr int ZP = HS + PER16;                             // pitch of z rows: 16 bytes more
-    constexpr bool LO = sizeof(T) == 2;
+    constexpr bool LO = sizeof(T) == 2, VEC = MODE == kFewWhole;
     constexpr int NV = 2;                                      // tiles of Vt a wave fetches ahead
     __shared__ float s_part[2][kFewWaves][kFewGroup][16 * EG + 1];
     __shared__ __attribute__((aligned(16))) float s_lf[2][kFewGroup][16 * EG];
@@ -167,7 +189,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
     const int nt = a.T - t0 < kFewGroup ? a.T - t0 : kFewGroup;
     const int slice = static_cast<int>(blockIdx.x) - routes;
     if (slice < 0) {
-        if (static_cast<int>(blockIdx.x) < nt) few_route<T, VEC>(a, t0 + blockIdx.x, s_lg, s_ex, s_idx[0]);
+        if (static_cast<int>(blockIdx.x) < nt) few_route<T, MODE>(a, t0 + blockIdx.x, s_lg, s_ex, s_idx[0]);
         return;
     }
     const int h0 = slice * HS;
@@ -199,19 +221,19 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
             const int e = 16 * g + row;
 #pragma unroll
             for (int i = 0; i < UN / HT; ++i)
-                gv[i] = few_load<T, VEC>(Wg + static_cast<int64_t>(e < E ? e : 0) * D, column(HT * i + ht), D, e < E);
+                gv[i] = few_pair<T, MODE>(Wg + static_cast<int64_t>(e < E ? e : 0) * D, column(HT * i + ht), D, e < E);
         };
 #pragma unroll
-        for (int i = 0; i < UN; ++i) wv[i] = few_load<T, VEC>(wrow, column(i), D, h < H);
+        for (int i = 0; i < UN; ++i) wv[i] = few_pair<T, MODE>(wrow, column(i), D, h < H);
 #pragma unroll
-        for (int i = 0; i < UN; ++i) xv[i] = few_load<T, VEC>(xrow, column(i), D, row < nt);
+        for (int i = 0; i < UN; ++i) xv[i] = few_pair<T, MODE>(xrow, column(i), D, row < nt);
         if (!a.routed) experts(0);
         if (s0 == kw) {
             // what the second half needs first, in flight with the rest
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int n = (wave + v * kFewWaves) * 16 + row;
-                vt[v] = few_load<T, VEC>(static_cast<const T*>(a.Vt) + static_cast<int64_t>(n < r ? n : 0) * H,
+                vt[v] = few_load<T, MODE>(static_cast<const T*>(a.Vt) + static_cast<int64_t>(n < r ? n : 0) * H,
                                          h0 + grp * PER16, H, n < r);
             }
         }
@@ -329,7 +351,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
         // the others again, in double
         for (unsigned left = s_unsure; left != 0; left &= left - 1) {
             const int t = __builtin_ctz(left);
-            few_logits<T, VEC>(a, x + static_cast<int64_t>(t) * D, wave, lane, s_lg);
+            few_logits<T, MODE>(a, x + static_cast<int64_t>(t) * D, wave, lane, s_lg);
             __syncthreads();
             if (tid < E) {
                 const int rank = few_rank(s_lg, E, tid);
@@ -396,7 +418,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
     };
     auto load = [&](const Tile& t, int s) {
         const bool in = t.row0 + row < t.n;
-        return few_load<T, VEC>(t.m + static_cast<int64_t>(in ? t.row0 + row : 0) * H, h0 + s * STEP + grp * PER16, H, in);
+        return few_load<T, MODE>(t.m + static_cast<int64_t>(in ? t.row0 + row : 0) * H, h0 + s * STEP + grp * PER16, H, in);
     };
     auto finish = [&](const Tile& t, const u32x4 (&v)[HS / STEP]) {
         f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -467,9 +489,10 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
 // US t + sum_j gate_j P u_j + b2 in float32.  Its time is two trips to memory
 // (routing and shares, the rows of US being fetched along with them; then P)
 // and the sum's.
-template <typename T, bool VEC>
+template <typename T, int MODE>
 __global__ __launch_bounds__(kOutThreads) void k_few_out(FewArgs a, int S, int rows) {
     constexpr int PER16 = Elem<T>::per16, SPAN = 16 * PER16;    // columns that 16 lanes read at once
+    constexpr bool VEC = MODE == kFewWhole;
     constexpr int W = VEC ? 4 : 1;                              // columns of the sums a thread takes
     constexpr int PU = 4;
     __shared__ __attribute__((aligned(16))) float s_red[kOutThreads * W];
@@ -489,7 +512,7 @@ __global__ __launch_bounds__(kOutThreads) void k_few_out(FewArgs a, int S, int r
     u32x4 us[PU];
 #pragma unroll
     for (int i = 0; i < PU; ++i)
-        us[i] = few_load<T, VEC>(static_cast<const T*>(a.US) + static_cast<int64_t>(d0 < d1 ? d0 : 0) * r,
+        us[i] = few_load<T, MODE>(static_cast<const T*>(a.US) + static_cast<int64_t>(d0 < d1 ? d0 : 0) * r,
                                  sub * PER16 + i * SPAN, r, d0 < d1);
     const float bias = a.b2 != nullptr && d0 < d1 ? a.b2[d0] : 0.0f;
     // and the first pieces of P for the first slots
@@ -499,7 +522,7 @@ __global__ __launch_bounds__(kOutThreads) void k_few_out(FewArgs a, int S, int r
     for (int j = 0; j < KS; ++j) {
         const int e = j < k ? idx[j] : -1;
         const bool in = d0 < d1 && e >= 0 && e < a.E;
-        ps[j] = few_load<T, VEC>(static_cast<const T*>(a.P) + (in ? static_cast<int64_t>(e) * D + d0 : 0) * q, sub * PER16, q, in);
+        ps[j] = few_load<T, MODE>(static_cast<const T*>(a.P) + (in ? static_cast<int64_t>(e) * D + d0 : 0) * q, sub * PER16, q, in);
     }
 
     // ---- the sums, S of them over G groups of threads
@@ -550,14 +573,14 @@ __global__ __launch_bounds__(kOutThreads) void k_few_out(FewArgs a, int S, int r
         if (d == d0)
 #pragma unroll
             for (int i = 0; i < PU; ++i) add(us[i], sub * PER16 + i * SPAN, r, 0);
-        for (int c = sub * PER16 + (d == d0 ? PU * SPAN : 0); c < r; c += SPAN) add(few_load<T, VEC>(row, c, r, in), c, r, 0);
+        for (int c = sub * PER16 + (d == d0 ? PU * SPAN : 0); c < r; c += SPAN) add(few_load<T, MODE>(row, c, r, in), c, r, 0);
         for (int j = 0; j < k; ++j) {
             const int e = idx[j];
             if (e < 0 || e >= a.E) continue;
             const T* p = static_cast<const T*>(a.P) + (static_cast<int64_t>(e) * D + (in ? d : 0)) * q;
             if (d == d0 && j < KS) add(j == 0 ? ps[0] : ps[1], sub * PER16, q, r + j * q);
             for (int c = sub * PER16 + (d == d0 && j < KS ? SPAN : 0); c < q; c += SPAN)
-                add(few_load<T, VEC>(p, c, q, in), c, q, r + j * q);
+                add(few_load<T, MODE>(p, c, q, in), c, q, r + j * q);
         }
 #pragma unroll
         for (int m = 8; m > 0; m >>= 1) v += __shfl_xor(v, m);
@@ -567,15 +590,15 @@ __global__ __launch_bounds__(kOutThreads) void k_few_out(FewArgs a, int S, int r
     }
 }
 
-template <typename T, bool VEC>
+template <typename T, int MODE>
 hipError_t few_hidden(const FewArgs& a, hipStream_t st) {
     const int routes = a.routed ? 0 : a.T < kFewGroup ? a.T : kFewGroup;
     const dim3 grid(few_slices(a.H) + routes, (a.T + kFewGroup - 1) / kFewGroup);
-    if (a.E <= 16) launch_kernel(k_few_hidden<T, VEC, 1, kSlice>, grid, dim3(kFewThreads), 0, st, a, routes);
-    else launch_kernel(k_few_hidden<T, VEC, 4, kSlice>, grid, dim3(kFewThreads), 0, st, a, routes);
+    if (a.E <= 16) launch_kernel(k_few_hidden<T, MODE, 1, kSlice>, grid, dim3(kFewThreads), 0, st, a, routes);
+    else launch_kernel(k_few_hidden<T, MODE, 4, kSlice>, grid, dim3(kFewThreads), 0, st, a, routes);
     return hipGetLastError();
 }
-template <typename T, bool VEC>
+template <typename T, int MODE>
 hipError_t few_out(const FewArgs& a, hipStream_t st) {
     // rows of y a workgroup: a wave's passes take four rows each, and every
     // workgroup sums all shares again, so there are about as many workgroups
@@ -585,7 +608,7 @@ hipError_t few_out(const FewArgs& a, hipStream_t st) {
     const int rows = ((a.D + most - 1) / most + pass - 1) / pass * pass;
     const dim3 grid(a.T, (a.D + rows - 1) / rows);
     const size_t lds = sizeof(float) * (a.r + static_cast<size_t>(a.k) * a.q);
-    launch_kernel(k_few_out<T, VEC>, grid, dim3(kOutThreads), lds > 0 ? lds : 4, st, a,
+    launch_kernel(k_few_out<T, MODE>, grid, dim3(kOutThreads), lds > 0 ? lds : 4, st, a,
                   few_slices(a.H), rows);
     return hipGetLastError();
 }
@@ -598,12 +621,17 @@ size_t few_part_bytes(int64_t T, int H, int r, int k, int q) {
            (static_cast<size_t>(r) + static_cast<size_t>(k) * static_cast<size_t>(q));
 }
 hipError_t launch_few_hidden(int dtype, bool whole, const FewArgs& a, hipStream_t st) {
-    if (dtype == 0) return whole ? few_hidden<float, true>(a, st) : few_hidden<float, false>(a, st);
-    return whole ? few_hidden<bf16_bits, true>(a, st) : few_hidden<bf16_bits, false>(a, st);
+    if (dtype == 0)
+        return whole                      ? few_hidden<float, kFewWhole>(a, st)
+               : a.D >= Elem<float>::per16 ? few_hidden<float, kFewPieces>(a, st)
+                                           : few_hidden<float, kFewElems>(a, st);
+    return whole                          ? few_hidden<bf16_bits, kFewWhole>(a, st)
+           : a.D >= Elem<bf16_bits>::per16 ? few_hidden<bf16_bits, kFewPieces>(a, st)
+                                           : few_hidden<bf16_bits, kFewElems>(a, st);
 }
 hipError_t launch_few_out(int dtype, bool whole, const FewArgs& a, hipStream_t st) {
-    if (dtype == 0) return whole ? few_out<float, true>(a, st) : few_out<float, false>(a, st);
-    return whole ? few_out<bf16_bits, true>(a, st) : few_out<bf16_bits, false>(a, st);
+    if (dtype == 0) return whole ? few_out<float, kFewWhole>(a, st) : few_out<float, kFewPieces>(a, st);
+    return whole ? few_out<bf16_bits, kFewWhole>(a, st) : few_out<bf16_bits, kFewPieces>(a, st);
 }
 
 }  // namespace clearmoe

@@ -748,11 +748,21 @@ __global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, 
                             for (int q = 0; q < 4; ++q)
                                 c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q8_widen<FB>(fb[s][j], q),
                                                                             q8_widen<FA>(fa[s][i], q), c, 0, 0, 0);
+                            // a lane's results are of the row that its A
+                            // fragment has; one factor for both scales unless
+                            // it is no normal number
                             if (s == 1) {
-                                // a lane's results are of the row that its A fragment has
-                                const float fa_ = q8_scale(sa[b & 1][i] & 255u), fb_ = q8_scale(sb[b & 1] & 255u);
+                                const uint32_t x = sa[b & 1][i] & 255u, y = sb[b & 1] & 255u;
+                                const int e = static_cast<int>(x + y) - 127;
+                                if (__ballot(e < 1 || e > 254 || x == 255u || y == 255u) == 0) {
+                                    const float f = __uint_as_float(static_cast<uint32_t>(e) << 23);
 #pragma unroll
-                                for (int v = 0; v < 16; ++v) acc[i][j][v] += c[v] * fa_ * fb_;
+                                    for (int v = 0; v < 16; ++v) acc[i][j][v] = __builtin_fmaf(c[v], f, acc[i][j][v]);
+                                } else {
+                                    const float fx = q8_scale(x), fy = q8_scale(y);
+#pragma unroll
+                                    for (int v = 0; v < 16; ++v) acc[i][j][v] += c[v] * fx * fy;
+                                }
                             }
                         } else {
                             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
@@ -825,7 +835,7 @@ hipError_t q8_formats(const Q8Desc& g, hipStream_t st) {
     if (g.out == kQ8OutF32) {
         if (q8_tiles(g, 16, 16) <= 800) return q8_rows<FA, FB, true>(g, st);
         if (q8_tiles(g, 64, 64) <= 1024) return q8_tile<2, 2, 1, 1, 4, FA, FB, kQ8OutF32>(g, st);
-        return q8_tile<4, 2, 1, 2, 4, FA, FB, kQ8OutF32>(g, st);
+        return q8_tile<4, 2, 2, 2, 2, FA, FB, kQ8OutF32>(g, st);
     }
     if (q8_tiles(g, 16, 16) <= 400) return q8_rows<FA, FB, false>(g, st);
     if (q8_tiles(g, 64, 64) <= 640) return q8_tile<2, 2, 1, 1, 4, FA, FB, kQ8OutBf16>(g, st);

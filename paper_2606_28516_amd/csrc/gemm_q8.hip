@@ -592,13 +592,16 @@ void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
     q8_epilogue<TM, TN, OUT, BM>(g, t, wave * 64, n0, 0, lane, smem + wave * (32 * 256), nullptr, nt_store != 0, acc);
 }
 
-// WM x WN waves of TM x TN MFMA tiles (32 x 32), NS stages in LDS: of each
-// stage the loads are issued NS - 1 stages ahead, so that the k loop runs at
-// the speed of its loads also where a CU has one workgroup and few of them.
-// Every stage's loads end with the scale words of its rows and columns.
+// KG groups of WM x WN waves of TM x TN MFMA tiles (32 x 32), NS stages in LDS
+// for each: of a stage the loads are issued NS - 1 stages ahead.  Every
+// stage's loads end with the scale words of its rows and columns.  The groups
+// take the stages in turn and their sums are added at the end: a workgroup
+// that is alone on its CU waits for one stage after the other, with two groups
+// for half as many (512 x 768 x 3072, 64 x 64 tiles: one group 10.3 us, two
+// 8.6, four 8.8; float32 17.6, 13.1, 12.5; more stages ahead change nothing).
 // WIDE: float32 results, on bfloat16 instructions (see above).
-template <int WM, int WN, int TM, int TN, int NS, int FA, int FB, int OUT>
-__global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
+template <int KG, int WM, int WN, int TM, int TN, int NS, int FA, int FB, int OUT>
+__global__ __launch_bounds__(64 * KG * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, int ntiles, int group, int nt_store) {
     constexpr bool WIDE = OUT == kQ8OutF32;
     constexpr int NW = WM * WN, SB = kGbRow, BM = WM * TM * 32, BN = WN * TN * 32, CPR = 8, BK = kQ8Block;
     constexpr int AL = BM / (8 * NW), BL = BN / (8 * NW), LPS = AL + BL + 1;
@@ -609,11 +612,13 @@ __global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, 
     constexpr int STAGE_A = BM * SB, STAGE = (BM + BN) * SB, SOFF = NS * STAGE, SSTAGE = 256 * NW;
     constexpr int EPI = NW * 32 * TN * 32 * (OUT == kQ8OutF32 ? 4 : OUT == kQ8OutBf16 ? 2 : 1);
     constexpr int SSIZE = NS * SSTAGE > WN * BM * 4 ? NS * SSTAGE : WN * BM * 4;
-    static_assert(SOFF >= EPI, "the epilogue's rows fit the stages");
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[SOFF + SSIZE + NW * 256];
+    constexpr int GROUP = SOFF + SSIZE, SUMS = NW * 64 * TM * TN * 64;
+    static_assert(SOFF >= EPI && (KG == 1 || SOFF >= SUMS), "the epilogue's rows and the sums fit the stages");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem_all[KG * GROUP + NW * 256];
 
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wave_all / NW, wave = wave_all % NW;
+    unsigned char* smem = smem_all + kg * GROUP;
     const int wm = wave / WN, wn = wave % WN;
     const int lrow = lane & 31, lh = lane >> 5, K = g.K;
 
@@ -621,6 +626,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, 
     if (!gb_tile<BM>(g, mtiles, ntiles, group, lane, t)) return;
     const int n0 = t.nt * BN;
     const int nk = static_cast<int>(q8_blocks(K)), left = K - (nk - 1) * BK;
+    const int steps = (nk + KG - 1) / KG;        // stage kg + KG * step is the group's
     const int lr = lane / CPR;
     // first k of the lane's chunk in an even load's 8 rows; odd: ^ 64
     const int kc0 = 16 * ((lane % CPR) ^ (lr >> 1));
@@ -661,7 +667,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, 
     // Stages past the last are issued too (zeros, no memory traffic), so that
     // every wait below counts the same.  Rows past the tile's lie past the
     // descriptor's end.
-    auto dma = [&](int kt, int b) {
+    auto dma = [&](int step, int b) {
+        const int kt = step * KG + kg;
         const bool past = kt >= nk;
         const int soff = __builtin_amdgcn_readfirstlane(past ? 0 : kt * BK);
 #pragma unroll
@@ -682,8 +689,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, 
                 __builtin_amdgcn_readfirstlane(lds0 + SOFF + b * SSTAGE + wave * 256));
     };
     // (a word a lane whatever TN is: 256 bytes)
-    constexpr int BOFF = SOFF + SSIZE;
-    if (g.bias != nullptr) q8_bias_dma<TN>(g, t.seg, n0 + wn * TN * 32, lane, lds0 + BOFF + wave * 256);
+    const uint32_t boff = KG * GROUP + wave * 256;
+    if (g.bias != nullptr && kg == 0) q8_bias_dma<TN>(g, t.seg, n0 + wn * TN * 32, lane, lds0 + boff);
 #pragma unroll
     for (int s = 0; s < NS; ++s) dma(s, s);
 
@@ -703,8 +710,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, 
 #pragma unroll
         for (int i = 0; i < TM; ++i) fa[s][i] = q8_lds_frag(smem + b * STAGE + i * 32 * SB, oa[s]);
     };
-    auto read_scales = [&](int kt, int b) {
-        const int sh = 8 * (kt & 3);
+    auto read_scales = [&](int step, int b) {
+        const int sh = 8 * ((step * KG + kg) & 3);
         const uint32_t* p = reinterpret_cast<const uint32_t*>(smem + SOFF + b * SSTAGE);
 #pragma unroll
         for (int i = 0; i < TM; ++i) sa[b & 1][i] = p[wm * TM * 32 + i * 32 + lrow] >> sh;
@@ -712,21 +719,21 @@ __global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, 
     };
     gb_wait_barrier<(NS - 1) * LPS>();           // the bias and stage 0 have landed
     f32x16 acc[TM][TN];
-    if (g.bias != nullptr) q8_start(lane, smem + BOFF + wave * 256, acc);
+    if (g.bias != nullptr && kg == 0) q8_start(lane, smem_all + boff, acc);
     else gb_zero(acc);
     read(0, 0);
     read_scales(0, 0);
     f32x16 part[WIDE ? TM : 1][WIDE ? TN : 1];
-    for (int k0 = 0; k0 < nk; k0 += NS) {
+    for (int k0 = 0; k0 < steps; k0 += NS) {
 #pragma unroll
         for (int b = 0; b < NS; ++b) {
             const int kt = k0 + b;
-            if (kt >= nk) break;
+            if (kt >= steps) break;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if (s == 0) {
                     read(b, 1);
-                } else if (kt + 1 < nk) {
+                } else if (kt + 1 < steps) {
                     // stage kt + 1 has landed for every wave, and every wave
                     // is done reading stage kt's buffer, which takes kt + NS
                     gb_wait_barrier<(NS - 2) * LPS>();
@@ -775,6 +782,37 @@ __global__ __launch_bounds__(64 * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, 
         }
     }
     gb_wait_barrier<0>();                        // the stage buffers are free
+    if constexpr (KG > 1) {
+        // the groups' sums, in order, through their own buffers
+        if (kg > 0)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<f32x4*>(smem + (((wave * TM + i) * TN + j) * 4 + q) * 1024 + lane * 16) =
+                            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __syncthreads();
+        if (kg > 0) {
+            // (the barrier of the first group's epilogue)
+            if constexpr (OUT != kQ8OutF32 && OUT != kQ8OutBf16 && TN < 4) __syncthreads();
+            return;
+        }
+#pragma unroll
+        for (int o = 1; o < KG; ++o)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 v = *reinterpret_cast<const f32x4*>(
+                            smem + o * GROUP + (((wave * TM + i) * TN + j) * 4 + q) * 1024 + lane * 16);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[i][j][4 * q + c] += v[c];
+                    }
+    }
     q8_epilogue<TM, TN, OUT, BM>(g, t, wm * TM * 32, n0 + wn * TN * 32, wn, lane, smem + wave * (EPI / NW),
                                  reinterpret_cast<float*>(smem + SOFF), nt_store != 0, acc);
 }
@@ -793,13 +831,13 @@ hipError_t q8_duo(const Q8Desc& g, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int WM, int WN, int TM, int TN, int NS, int FA, int FB, int OUT>
+template <int KG, int WM, int WN, int TM, int TN, int NS, int FA, int FB, int OUT>
 hipError_t q8_tile(const Q8Desc& g, hipStream_t st) {
     constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
     const int64_t mt = (g.M + BM - 1) / BM + (g.seg_offsets != nullptr ? g.nseg : 0), nt = (g.N + BN - 1) / BN;
     const int64_t grid = (mt * nt + kGbXcds - 1) / kGbXcds * kGbXcds;
     const int64_t bytes = g.M * g.N * (OUT == kQ8OutF32 ? 4 : OUT == kQ8OutBf16 ? 2 : 1);
-    launch_kernel(k_q8_tile<WM, WN, TM, TN, NS, FA, FB, OUT>, dim3(static_cast<unsigned>(grid)), dim3(64 * WM * WN), 0,
+    launch_kernel(k_q8_tile<KG, WM, WN, TM, TN, NS, FA, FB, OUT>, dim3(static_cast<unsigned>(grid)), dim3(64 * KG * WM * WN), 0,
                   st, g, static_cast<int>(mt), static_cast<int>(nt), 4, bytes >= kQ8StreamBytes ? 1 : 0);
     return hipGetLastError();
 }
@@ -814,13 +852,13 @@ int64_t q8_tiles(const Q8Desc& g, int bm, int bn) {
 // chip.  Times in us on an MI355X, N x K of 768 x 3072 and 384 x 1536 to
 // bfloat16 and float32, 3072 x 768 and 1536 x 384 with GELU to 8 bits:
 //                    rows of A   128        1024         4096         16384
-//   bfloat16  16 x 16 (rows)   8.6  4.7  38.0  11.8   141   39
-//             64 x 64          9.2  6.4  10.1   6.7    22.1  8.9     80   24
+//   bfloat16  16 x 16 (rows)   8.6  4.5  38.0  11.8   141   39
+//             64 x 64          8.4  6.0   9.0   6.3    22.9  9.1     80   24
 //             128 x 128       15.6  9.7  16.5  10.1    19.1 10.8     56   22
 //             256 x 128 (duo) 28.3 16.3  29.4  16.7    32.9 17.3     42   21
-//   float32   16 x 16          9.3        39.4        143
-//             64 x 64         17.6        18.7         39.2         136
-//             128 x 128       32.5        33.5         36.9         108
+//   float32   16 x 16          9.4        39.4        143
+//             64 x 64         12.7        13.9         32.5
+//             256 x 128                                38.3         108
 //   8 bits    64 x 128         7.2  6.0   9.6   6.2    25.1 11.9     89   35
 //             256 x 128 (duo) 12.8  9.6  13.4  10.0    20.5 11.0     57   25
 template <int FA, int FB>
@@ -829,17 +867,17 @@ hipError_t q8_formats(const Q8Desc& g, hipStream_t st) {
         // two workgroups of 64 x 128 on every CU, or more rows a workgroup
         const bool few = q8_tiles(g, 64, 128) <= 512;
         if (g.out == kQ8OutE4M3)
-            return few ? q8_tile<2, 2, 1, 2, 2, FA, FB, kQ8OutE4M3>(g, st) : q8_duo<FA, FB, kQ8OutE4M3>(g, st);
-        return few ? q8_tile<2, 2, 1, 2, 2, FA, FB, kQ8OutE5M2>(g, st) : q8_duo<FA, FB, kQ8OutE5M2>(g, st);
+            return few ? q8_tile<1, 2, 2, 1, 2, 2, FA, FB, kQ8OutE4M3>(g, st) : q8_duo<FA, FB, kQ8OutE4M3>(g, st);
+        return few ? q8_tile<1, 2, 2, 1, 2, 2, FA, FB, kQ8OutE5M2>(g, st) : q8_duo<FA, FB, kQ8OutE5M2>(g, st);
     }
     if (g.out == kQ8OutF32) {
         if (q8_tiles(g, 16, 16) <= 800) return q8_rows<FA, FB, true>(g, st);
-        if (q8_tiles(g, 64, 64) <= 1024) return q8_tile<2, 2, 1, 1, 4, FA, FB, kQ8OutF32>(g, st);
-        return q8_tile<4, 2, 2, 2, 2, FA, FB, kQ8OutF32>(g, st);
+        if (q8_tiles(g, 64, 64) <= 1024) return q8_tile<2, 2, 2, 1, 1, 2, FA, FB, kQ8OutF32>(g, st);
+        return q8_tile<1, 4, 2, 2, 2, 2, FA, FB, kQ8OutF32>(g, st);
     }
     if (q8_tiles(g, 16, 16) <= 400) return q8_rows<FA, FB, false>(g, st);
-    if (q8_tiles(g, 64, 64) <= 640) return q8_tile<2, 2, 1, 1, 4, FA, FB, kQ8OutBf16>(g, st);
-    if (q8_tiles(g, 256, 128) < 192) return q8_tile<4, 2, 1, 2, 4, FA, FB, kQ8OutBf16>(g, st);
+    if (q8_tiles(g, 64, 64) <= 640) return q8_tile<2, 2, 2, 1, 1, 2, FA, FB, kQ8OutBf16>(g, st);
+    if (q8_tiles(g, 256, 128) < 192) return q8_tile<1, 4, 2, 1, 2, 4, FA, FB, kQ8OutBf16>(g, st);
     return q8_duo<FA, FB, kQ8OutBf16>(g, st);
 }
 

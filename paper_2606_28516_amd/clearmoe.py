@@ -203,6 +203,19 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+def _shaped(t: torch.Tensor, dtype, shape: tuple, what: str) -> int:
+    """The address of a tensor that has to have this type and shape."""
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not dtype or t.shape != shape:
+        raise ClearMoEError(f"{what} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _shaped_or_none(t: Optional[torch.Tensor], dtype, shape: tuple, what: str) -> Optional[int]:
+    return None if t is None else _shaped(t, dtype, shape, what)
+
+
 def _queue(x: torch.Tensor, stream) -> int:
     """The stream of a call on x's device, which has to be the current one: the
     kernels are launched there.  The current stream is asked for by its handle
@@ -459,11 +472,20 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
     """clearmoe_ffn_forward_few: the whole layer for at most FEW_MAX_TOKENS
     tokens, with any router without class tokens.  Returns y."""
     T, D = x.shape
-    E, _, q = P.shape
-    s = Shape(T, D, W1.shape[0], E, k, US.shape[1], q, _dt(x), renorm)
+    H, r, (E, _, q), dt = W1.shape[0], US.shape[1], P.shape, x.dtype
+    s = Shape(T, D, H, E, k, r, q, _dt(x), renorm)
+    f32 = torch.float32
+    y = torch.empty_like(x) if out is None else out
+    # (one expression: a check a tensor would cost a small call 2 us)
+    if not (W1.dtype is US.dtype is Vt.dtype is P.dtype is Q.dtype is y.dtype is dt and W1.shape == (H, D)
+            and US.shape == (D, r) and Vt.shape == (r, H) and P.shape == (E, D, q) and Q.shape == (E, q, H)
+            and y.numel() == T * D and (b1 is None or (b1.numel() == H and b1.dtype is f32))
+            and (b2 is None or (b2.numel() == D and b2.dtype is f32))
+            and (idx_out is None or (idx_out.numel() == T * k and idx_out.dtype is torch.int32))
+            and (gate_out is None or (gate_out.numel() == T * k and gate_out.dtype is f32))):
+        raise ClearMoEError(f"the tensors do not fit x [{T}, {D}] {dt}, W1 [{H}, .], US [., {r}] and P [{E}, ., {q}]")
     xp, st = _ptr(x), _queue(x, stream)
     ws = alloc_few_workspace(s, x.device) if ws is None else ws
-    y = torch.empty_like(x) if out is None else out
     rc = lib().clearmoe_ffn_forward_few(ctypes.byref(s), ctypes.byref(router), xp, _ptr(W1),
                                         _ptr(b1), _ptr(US), _ptr(Vt), _ptr(b2), _ptr(P), _ptr(Q), _ptr(y),
                                         _ptr(idx_out), _ptr(gate_out), _ptr(ws), ws.numel(), st)
@@ -488,17 +510,6 @@ def _value_cols(cols: int) -> int:
 
 def _scale_cols(cols: int) -> int:
     return (cols + 511) // 512 * 4
-
-
-def _shaped(t: torch.Tensor, dtype, shape: tuple, what: str) -> int:
-    """The address of a tensor that has to have this type and shape."""
-    if t.dtype is not dtype or t.shape != shape:
-        raise ClearMoEError(f"{what} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
-
-
-def _shaped_or_none(t: Optional[torch.Tensor], dtype, shape: tuple, what: str) -> Optional[int]:
-    return None if t is None else _shaped(t, dtype, shape, what)
 
 
 def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):

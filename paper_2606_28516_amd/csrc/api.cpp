@@ -1539,7 +1539,7 @@ FewLayout few_layout(const clearmoe_shape& s) {
 
 struct QuantizedLayout {
     size_t xv, xs, zv, zs;     // x and z quantised
-    size_t z;                  // or z in float32, where every workgroup quantises the few rows itself
+    size_t z;                  // or (at 0) z in float32, where every workgroup quantises the few rows itself
     size_t total;
 };
 bool quantized_few(const clearmoe_shape& s) {
@@ -1553,16 +1553,15 @@ QuantizedLayout quantized_layout(const clearmoe_shape& s) {
         off += up(static_cast<size_t>(s.T) * static_cast<size_t>(bytes) + 1);
         return at;
     };
-    if (quantized_few(s)) {
-        L.z = take(static_cast<int64_t>(sizeof(float)) * s.H);
-        L.total = off;
-        return L;
-    }
     L.xv = take(q8_cols(s.D));
     L.xs = take(q8_scale_cols(s.D));
     L.zv = take(q8_cols(s.H));
     L.zs = take(q8_scale_cols(s.H));
-    L.total = off;
+    // z in float32 takes the same bytes; a workspace for more rows also holds
+    // any number of few ones
+    const size_t few = static_cast<size_t>(s.T < kQ8FewRows ? s.T : kQ8FewRows);
+    const size_t z = up(sizeof(float) * few * static_cast<size_t>(s.H) + 1);
+    L.total = off > z ? off : z;
     return L;
 }
 bool byte_format(int f) { return f == CLEARMOE_E4M3 || f == CLEARMOE_E5M2; }

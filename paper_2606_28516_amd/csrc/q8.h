@@ -123,6 +123,7 @@ hipError_t launch_gemm_q8(const Q8Desc& g, hipStream_t st);
 // quantises its rows of A itself, in blocks of 128 columns, so that a
 // quantising pass over them is not a launch of its own.  float32 or bfloat16
 // results; SA, A, lda, fa and fb are not used.
+constexpr int64_t kQ8FewRows = 16;       // at most: then a pass of its own costs less
 bool q8_few_supported(int64_t M, int64_t K);
 hipError_t launch_q8_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStream_t st);
 

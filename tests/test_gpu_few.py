@@ -267,6 +267,40 @@ def test_streams_graphs_and_a_shared_workspace():
                 assert torch.equal(a, b), i
 
 
+def test_mismatched_tensors_are_refused():
+    L = _layer(4, 64, 128, 4, 2, 16, 8, BF16, 7)
+    rt = _router(L)
+    for name, bad in (("W1", L["W1"][:, :32]), ("US", L["US"][:32].contiguous()), ("Vt", L["Vt"][:8].contiguous()),
+                      ("Q", L["Q"][:3].contiguous()), ("b1", L["b1"][:5]), ("W1", L["W1"].float()),
+                      ("P", L["P"].transpose(1, 2))):
+        with pytest.raises(cm.ClearMoEError):
+            _few({**L, name: bad}, rt)
+    for kw in (dict(out=torch.empty(4, 63, dtype=BF16, device="cuda")), dict(out=torch.empty(4, 64, device="cuda")),
+               dict(ws=torch.empty(8, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(cm.ClearMoEError):
+            _few(L, rt, **kw)
+
+
+def test_two_streams_at_once():
+    """Calls that overlap in time, each with a workspace of its own."""
+    L = _layer(16, 768, 1536, 8, 2, 256, 64, BF16, 3)
+    rt = _router(L)
+    want = _few(L, rt)
+    n = cm.few_workspace_bytes(cm.make_shape(16, 768, 8, 2, cm.BF16, H=1536, r=256, q=64))
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in streams]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for st, w in zip(streams, ws):
+            with torch.cuda.stream(st):
+                got.append(_few(L, rt, ws=w))
+    torch.cuda.synchronize()
+    for g in got:
+        for a, b in zip(g, want):
+            assert torch.equal(a, b)
+
+
 def test_no_tokens_and_too_many():
     L = _layer(65, 64, 128, 4, 2, 16, 8, BF16, 7)
     rt = _router(L)

@@ -299,6 +299,71 @@ def test_product_nan_and_infinity_stay_in_their_row(out):
     assert torch.equal(c[keep], want[keep])
 
 
+@pytest.mark.parametrize("M", [20, 9000])
+@pytest.mark.parametrize("out", FMTS)
+def test_product_to_bytes_with_infinities(out, M):
+    """Infinite and NaN results: NaN in e4m3, infinity kept in e5m2; the block's
+    scale is that of the finite ones."""
+    N, K = 400, 64
+    g = _gen(14)
+    a, sa, _ = _operand(g, (M, K), E4M3, 1)
+    b, sb, _ = _operand(g, (N, K), E4M3, 128)
+    bias = torch.zeros(N, device="cuda")
+    want, ws = cm.quantized_gemm(a, sa, b, sb, bias=bias, out_dtype=out)
+    bias[7], bias[200], bias[399] = math.inf, -math.inf, math.nan
+    got, gs = cm.quantized_gemm(a, sa, b, sb, bias=bias, out_dtype=out)
+    f = got.float()
+    assert f[:, 399].isnan().all()
+    if out == E4M3:
+        assert f[:, 7].isnan().all() and f[:, 200].isnan().all()
+    else:
+        assert (f[:, 7] == math.inf).all() and (f[:, 200] == -math.inf).all()
+    keep = [n for n in range(N) if n not in (7, 200, 399)]
+    assert f[:, keep].isfinite().all()
+    same = (gs.view(torch.uint8) == ws.view(torch.uint8))[:, :4]
+    assert same.float().mean() > 0.9              # the largest of a block was rarely one of the three
+    for i in range(4):
+        cols = [n for n in keep if n // 128 == i]
+        rows = same[:, i]
+        assert torch.equal(f[rows][:, cols], want.float()[rows][:, cols])
+
+
+def test_workspace_of_more_rows_holds_fewer():
+    D, H = 72, 1000
+    x, W1, b1, W2, b2 = _ffn_inputs(40, D, H, 0, torch.bfloat16, 3)
+    w1, s1 = cm.quantize(W1.cuda(), block_rows=128)
+    w2, s2 = cm.quantize(W2.cuda(), block_rows=128)
+    last = 0
+    for T in range(1, 41):
+        n = cm.quantized_workspace_bytes(cm.make_shape(T, D, 1, 1, cm.BF16, H=H))
+        assert n >= last
+        last = n
+    ws = cm.alloc_quantized_workspace(cm.make_shape(17, D, 1, 1, cm.BF16, H=H))
+    for T in (1, 9, 16, 17):
+        xt = x[:T].contiguous().cuda()
+        y = cm.quantized_ffn_forward(xt, w1, s1, b1.cuda(), w2, s2, b2.cuda(), ws=ws)
+        assert torch.equal(y, cm.quantized_ffn_forward(xt, w1, s1, b1.cuda(), w2, s2, b2.cuda()))
+
+
+def test_mismatched_tensors_are_refused():
+    g = _gen(15)
+    a, sa, _ = _operand(g, (6, 64), E4M3, 1)
+    b, sb, _ = _operand(g, (40, 64), E4M3, 128)
+    ok = dict(bias=torch.zeros(40, device="cuda"))
+    cm.quantized_gemm(a, sa, b, sb, **ok)
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for args, kw in (((a, sa[:5], b, sb), {}), ((a, sa, b, sb.repeat(2, 1)), {}), ((a, sa, b[:, :48].contiguous(), sb), {}),
+                     ((a, sa, b, sb), dict(bias=torch.zeros(39, device="cuda"))),
+                     ((a, sa, b, sb), dict(bias=torch.zeros(40, device="cuda").double())),
+                     ((a, sa, b, sb), dict(offsets=off)),
+                     ((a, sa, b[None], sb[None]), dict(offsets=off)),
+                     ((a, sa.view(torch.uint8), b, sb), {}), ((a.float(), sa, b, sb), {}),
+                     ((a, sa, b, sb), dict(out=torch.empty(6, 41, dtype=torch.bfloat16, device="cuda"))),
+                     ((a, sa, b, sb), dict(out_dtype=torch.float16))):
+        with pytest.raises(cm.ClearMoEError):
+            cm.quantized_gemm(*args, **kw)
+
+
 def test_product_row_strides():
     """lda and ldc through the C ABI: rows inside wider arrays, whose other
     bytes stay as they were."""
@@ -382,7 +447,7 @@ def test_ffn(T, D, H, dtype):
 
 
 @pytest.mark.parametrize("T,D,H,offsets", [
-    (7, 64, 256, [0, 1, 1, 7]), (40, 100, 390, [2, 20, 30]), (700, 192, 512, [0, 300, 301, 301, 650]),
+    (7, 64, 256, [0, 1, 1, 7]), (12, 72, 264, [2, 5, 9]), (40, 100, 390, [2, 20, 30]), (700, 192, 512, [0, 300, 301, 301, 650]),
     (1000, 256, 1030, [0, 250, 480, 770, 1000])])
 def test_ffn_groups(T, D, H, offsets):
     E = len(offsets) - 1
@@ -401,11 +466,12 @@ def test_ffn_groups(T, D, H, offsets):
     assert (y[:offsets[0]] == 7.5).all() and (y[offsets[-1]:] == 7.5).all()
 
 
-def test_experts_between_dispatch_and_combine():
+@pytest.mark.parametrize("T", [200, 7])
+def test_experts_between_dispatch_and_combine(T):
     """Route, dispatch with rows, the experts' 8-bit FFN, combine: the layer of
     a caller's own experts, eager and as a captured graph on another stream,
     replayed with other inputs and eager calls in between."""
-    T, D, H, E, k = 200, 128, 320, 5, 2
+    D, H, E, k = 128, 320, 5, 2
     x, W1, b1, W2, b2 = _ffn_inputs(T, D, H, E, torch.bfloat16, 21)
     g = _gen(22)
     Wg, bg = torch.randn(E, D, generator=g).bfloat16(), 0.1 * torch.randn(E, generator=g)

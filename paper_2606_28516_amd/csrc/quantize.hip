@@ -1,7 +1,10 @@
 // 8-bit floating point with power-of-two block scales (q8.h).  The scale is
 // exact to divide by, so a value is rounded once, and the matrix instructions
 // apply it for nothing.  One read of x, one write of its bytes: bound by
-// memory.
+// memory.  Measured on an MI355X: rows of 50432 x 768 bfloat16 in 25 us (4.7
+// TB/s; a large copy moves 4.8), 12608 x 384 in 5, squares of 8 x 1550 x 790
+// float32 in 15 (3.2 TB/s: a workgroup holds its square until the maximum of
+// all of it is known).
 #include "q8.h"
 
 namespace clearmoe {

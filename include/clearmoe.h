@@ -317,9 +317,9 @@ int clearmoe_dense_ffn_forward(const clearmoe_shape* shape, const void* x, const
  * kernels whose time hardly depends on the token count: the form for serving
  * single tokens and small batches.
  *   - Any router but one with class tokens (dense_stride > 0:
- *     CLEARMOE_ERR_UNSUPPORTED).  Linear routers run inside the first kernel,
- *     every logit in double; an MLP router runs before it, as
- *     clearmoe_route_ex.
+ *     CLEARMOE_ERR_UNSUPPORTED).  Linear routers run inside the first kernel:
+ *     gates from logits in double, and the experts that those choose; an MLP
+ *     router runs before it, as clearmoe_route_ex.
  *   - Any D, H, r, q (r + k q <= 12288, else CLEARMOE_ERR_UNSUPPORTED); where
  *     all are multiples of 8 (bf16) or 4 (float32) and every tensor is 16-byte
  *     aligned, memory is read in 16-byte pieces, else element by element, for

@@ -62,9 +62,18 @@ __device__ __forceinline__ bf16x8 q8_widen(const i32x8& f, int i) {
     }
     return v;
 }
-// The scale a byte stands for.
-__device__ __forceinline__ float q8_scale(uint32_t b) {
-    return b == 0 ? 0x1p-127f : b == 255 ? __builtin_nanf("") : __uint_as_float(b << 23);
+// acc + c 2^(x - 127) 2^(y - 127): a block's sum c and the scale bytes of its
+// operands.  The exponents are added before anything is multiplied: one scale
+// may be so large or small that c times it alone leaves float32's range though
+// the result is an ordinary number.  Where the two are no normal factor
+// together, c's own exponent is moved.  What a result is depends on its own
+// scales alone, not on the kernel or on the rows beside it.
+__device__ __forceinline__ float q8_add_scaled(float acc, float c, uint32_t x, uint32_t y) {
+    const int e = static_cast<int>(x + y) - kQ8One;
+    const bool normal = e >= 1 && e <= 254;
+    const float by_factor = __builtin_fmaf(c, __uint_as_float(static_cast<uint32_t>(normal ? e : 1) << 23), acc);
+    const float r = normal ? by_factor : acc + __builtin_ldexpf(c, e - kQ8One);
+    return x == 255u || y == 255u ? __builtin_nanf("") : r;
 }
 
 // Eight waves share the sum, since there are few tiles and each waits for its
@@ -94,10 +103,13 @@ __global__ __launch_bounds__(512) void k_q8_rows(Q8Desc g, int mtiles, int ntile
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q8_widen<FB>(fb, i), q8_widen<FA>(fa, i), c, 0, 0, 0);
+            // (kept in front of what depends on a lane's scales: all lanes take
+            // part in a matrix instruction)
+            asm volatile("" : "+v"(c));
             // a lane's results are of the row that its A fragment has
-            const float ka = q8_scale(sa[kb]), kb_ = q8_scale(sb[kb]);
+            const uint32_t x = sa[kb], y = sb[kb];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] += c[v] * ka * kb_;
+            for (int v = 0; v < 4; ++v) acc[v] = q8_add_scaled(acc[v], c[v], x, y);
         } else {
             acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa, acc, FB, FA, 0, sb[kb], 0, sa[kb]);
         }
@@ -182,9 +194,10 @@ __global__ __launch_bounds__(512) void k_q8_few(Q8Desc g, const TA* A, int K0, i
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q8_widen<kQ8E4M3>(b, i), q8_widen<kQ8E4M3>(a, i), c, 0, 0, 0);
-            const float ka = q8_scale(sa), kb_ = q8_scale(scale);
+            asm volatile("" : "+v"(c));
 #pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] += c[v] * ka * kb_;
+            for (int v = 0; v < 4; ++v)
+                acc[v] = q8_add_scaled(acc[v], c[v], static_cast<uint32_t>(sa), static_cast<uint32_t>(scale));
         } else {
             acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, kQ8E4M3, kQ8E4M3, 0, scale, 0, sa);
         }
@@ -778,9 +791,8 @@ __global__ __launch_bounds__(64 * KG * WM * WN) void k_q8_tile(Q8Desc g, int mti
 #pragma unroll
                                     for (int v = 0; v < 16; ++v) acc[i][j][v] = __builtin_fmaf(c[v], f, acc[i][j][v]);
                                 } else {
-                                    const float fx = q8_scale(x), fy = q8_scale(y);
 #pragma unroll
-                                    for (int v = 0; v < 16; ++v) acc[i][j][v] += c[v] * fx * fy;
+                                    for (int v = 0; v < 16; ++v) acc[i][j][v] = q8_add_scaled(acc[i][j][v], c[v], x, y);
                                 }
                             }
                         } else {

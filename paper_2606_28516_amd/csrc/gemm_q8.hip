@@ -341,6 +341,7 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
     static_assert(RB >= 32 && 64 % CH == 0 && 32 % RPI == 0, "whole rows per store");
     const int lrow = lane & 31, lh = lane >> 5;
     const int cols = static_cast<int>(q8_cols(g.N));
+    const bool cut = cols != g.N;                // the last 16 bytes of a row hold bytes past N
     if (g.gelu)
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -458,8 +459,18 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
                 }
             } else {
                 const int n = nw + ch * 16;
-                if (n < cols)
-                    *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(g.C) + (t.m_lo + rl) * g.ldc + n) = w;
+                if (n >= cols) continue;
+                u32x4 o = w;
+                if (cut && n + 16 > g.N) {
+                    // bytes past N are zeros whatever the row holds (their sums
+                    // are zeros times A, NaN where A is no number or infinite)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int keep = g.N - n - 4 * q;
+                        o[q] = keep >= 4 ? w[q] : keep <= 0 ? 0u : w[q] & ((1u << (8 * keep)) - 1u);
+                    }
+                }
+                *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(g.C) + (t.m_lo + rl) * g.ldc + n) = o;
             }
         }
         __builtin_amdgcn_wave_barrier();

@@ -85,6 +85,12 @@ __device__ __forceinline__ int gb_incl_scan(int v) {
     return v;
 }
 
+// Row tiles of bm rows that a segment takes (unsigned: of almost 2^31 rows the
+// sum would pass an int).
+__host__ __device__ constexpr int gb_row_tiles(int rows, int bm) {
+    return static_cast<int>((static_cast<uint32_t>(rows) + static_cast<uint32_t>(bm - 1)) / static_cast<uint32_t>(bm));
+}
+
 // What a workgroup works on: rows [m_lo, m_lo + rows) of segment seg, column
 // tile nt.
 struct GbTile {
@@ -133,7 +139,7 @@ __device__ __forceinline__ bool gb_tile(const Desc& g, int mtiles, int ntiles, i
         int lo = lane < g.nseg ? g.seg_offsets[lane] : 0, hi = lane < g.nseg ? g.seg_offsets[lane + 1] : 0;
         lo = lo < 0 ? 0 : (lo > M ? M : lo);
         hi = hi < lo ? lo : (hi > M ? M : hi);
-        const int n_t = (hi - lo + BM - 1) / BM;
+        const int n_t = gb_row_tiles(hi - lo, BM);
         const int tend = gb_incl_scan(n_t);
         const uint64_t hit = __ballot(lane < g.nseg && mt < tend);
         if (hit == 0) return false;

@@ -42,3 +42,26 @@ def test_bytes_past_the_columns_are_zero(M, N, K, out, gelu):
     assert (~got.float()[bad, :N].isfinite()).all()
     assert torch.equal(got.view(torch.uint8)[keep], want.view(torch.uint8)[keep])
     assert torch.equal(gs.view(torch.uint8)[keep], ws.view(torch.uint8)[keep])
+
+
+# ---------------------------------------------------------------------------
+# As many rows as a product may have
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("last", [0, 100])
+def test_a_group_of_almost_2_31_rows(last):
+    M, N, K = 2 ** 31 - 1, 1, 16
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB of device memory")
+    E = 2 if last else 1
+    a = torch.full((M, K), 0x38, dtype=torch.uint8, device="cuda").view(E4M3)            # ones
+    sa = torch.full((M, 4), 127, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+    b = torch.full((E, N, K), 0x38, dtype=torch.uint8, device="cuda").view(E4M3)
+    sb = torch.full((E, 1, 4), 127, dtype=torch.uint8, device="cuda")
+    sb[-1] += 1 if last else 0                                                           # the last expert's: twos
+    out = torch.full((M, N), 7.5, dtype=BF16, device="cuda")
+    off = torch.tensor([0, M - last, M][:E] + [M], dtype=torch.int32, device="cuda")
+    cm.quantized_gemm(a, sa, b, sb.view(torch.float8_e8m0fnu), offsets=off, out=out)
+    right = int((out[:M - last] == 16).sum()), int((out[M - last:] == 32).sum())
+    del a, sa, out
+    torch.cuda.empty_cache()
+    assert right == (M - last, last)

@@ -361,7 +361,8 @@ typedef enum { CLEARMOE_E4M3 = 2, CLEARMOE_E5M2 = 3 } clearmoe_byte_format;
  * infinity stays itself.  Bytes past cols are written as 0, scales past the
  * last block as 1.  Pointers: x element-aligned (rows that start at 16-byte
  * boundaries are read fastest), values 16-byte, scales 4-byte aligned.
- * 1 <= cols <= 65536. */
+ * 1 <= cols <= 65536; batch and rows below 2^31, ldx at most 2^40, and at most
+ * 2^31 blocks in all (a block for each scale). */
 int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int64_t rows,
                       int32_t cols, const void* x, int64_t ldx, void* values, void* scales,
                       hipStream_t stream);

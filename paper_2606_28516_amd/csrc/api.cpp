@@ -1633,8 +1633,7 @@ int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int6
     if (block_rows != 1 && block_rows != kQ8Block) return CLEARMOE_ERR_INVALID_ARG;
     if (cols < 1 || cols > kMaxDim || batch < 0 || rows < 0 || ldx < cols) return CLEARMOE_ERR_INVALID_ARG;
     if (batch == 0 || rows == 0) return CLEARMOE_OK;
-    // one workgroup for 16 row blocks or for a 128 x 128 block: the grid's
-    // limit, checked so that no product overflows
+    // (checked so that no product overflows)
     constexpr int64_t kMostBlocks = int64_t{1} << 31;
     if (rows >= kMostBlocks || batch >= kMostBlocks || ldx > (int64_t{1} << 40)) return CLEARMOE_ERR_INVALID_ARG;
     const int64_t per = block_rows == 1 ? rows : (rows + kQ8Block - 1) / kQ8Block;

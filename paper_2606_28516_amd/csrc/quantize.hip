@@ -38,17 +38,17 @@ __global__ __launch_bounds__(kThreads) void k_quantize_rows(const T* x, int64_t 
     }
 }
 
-// 128 x 128 blocks: a workgroup each, its values in registers between the
-// maximum and the rounding.
+// 128 x 128 blocks: a workgroup each (from block `first` on), its values in
+// registers between the maximum and the rounding.
 template <typename T, int FMT>
 __global__ __launch_bounds__(kThreads) void k_quantize_square(const T* x, int64_t ldx, int64_t rows, int64_t cols,
-                                                              uint8_t* v, uint8_t* scale) {
+                                                              int64_t first, uint8_t* v, uint8_t* scale) {
     constexpr int PASS = kThreads / kLanes, NP = kQ8Block / PASS;       // rows a pass, passes
     __shared__ float s_m[kThreads / 64];
     const int64_t blocks = q8_blocks(cols), vcols = q8_cols(cols), scols = q8_scale_cols(cols);
     const int64_t nr = (rows + kQ8Block - 1) / kQ8Block;
     const int sub = threadIdx.x % kLanes, rl = threadIdx.x / kLanes;
-    const int64_t blk = blockIdx.x % blocks, br = blockIdx.x / blocks;  // row block over all batches
+    const int64_t at = first + blockIdx.x, br = at / blocks, blk = at - br * blocks;    // row block over all batches
     const int64_t batch = br / nr, r0 = (br - batch * nr) * kQ8Block, c = blk * kQ8Block + sub * 8;
     const T* xb = x + batch * rows * ldx;
     float f[NP][8], m = 0.0f;
@@ -81,18 +81,29 @@ __global__ __launch_bounds__(kThreads) void k_quantize_square(const T* x, int64_
     }
 }
 
+// Workgroups of a launch: a grid holds less than 2^32 threads.  Larger
+// matrices take several launches.
+constexpr int64_t kMostGroups = ((int64_t{1} << 32) - 1) / kThreads;
+
 template <typename T, int FMT>
 hipError_t quantize(int block_rows, int64_t batch, int64_t rows, int64_t cols, const T* x, int64_t ldx, uint8_t* v,
                     uint8_t* scale, hipStream_t st) {
+    constexpr int64_t PER = kThreads / kLanes;                          // row blocks a workgroup
     const int64_t blocks = q8_blocks(cols);
     if (block_rows == 1) {
-        const int64_t n = batch * rows * blocks, grid = (n + kThreads / kLanes - 1) / (kThreads / kLanes);
-        launch_kernel(k_quantize_rows<T, FMT>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st, x, ldx,
-                      batch * rows, cols, v, scale);
+        const int64_t all = batch * rows, most = kMostGroups * PER / blocks;
+        for (int64_t r = 0; r < all; r += most) {
+            const int64_t n = all - r < most ? all - r : most, grid = (n * blocks + PER - 1) / PER;
+            launch_kernel(k_quantize_rows<T, FMT>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st,
+                          x + r * ldx, ldx, n, cols, v + r * q8_cols(cols), scale + r * q8_scale_cols(cols));
+        }
     } else {
-        const int64_t grid = batch * ((rows + kQ8Block - 1) / kQ8Block) * blocks;
-        launch_kernel(k_quantize_square<T, FMT>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st, x, ldx,
-                      rows, cols, v, scale);
+        const int64_t all = batch * ((rows + kQ8Block - 1) / kQ8Block) * blocks;
+        for (int64_t b = 0; b < all; b += kMostGroups) {
+            const int64_t grid = all - b < kMostGroups ? all - b : kMostGroups;
+            launch_kernel(k_quantize_square<T, FMT>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st, x, ldx,
+                          rows, cols, b, v, scale);
+        }
     }
     return hipGetLastError();
 }

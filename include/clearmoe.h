@@ -370,9 +370,10 @@ int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int6
 /* A product C = epi(A B^T + bias) of quantised matrices, A [M, K] with row
  * scales and B [N, K] with 128 x 128 scales, summed in float32 from the first
  * to the last block.
- *   M, N, K    0 <= M < 2^31; N, K in 1 .. 65536, M N <= 2^44, K a multiple of
- *              16 (the width of the value rows: zeros past the columns add
- *              nothing).
+ *   M, N, K    0 <= M < 2^31; N, K in 1 .. 65536, K a multiple of 16 (the width
+ *              of the value rows: zeros past the columns add nothing); what one
+ *              launch holds: (ceil(M / 256) + groups) ceil(N / 128) at most
+ *              2^24 - 8, for F32 results 2^23 - 8.
  *   groups     0: one B.  E (1 .. 64): B [E, N, K], scales [E, ceil(N / 128), .]
  *              and bias [E, N], one for each expert; rows offsets[e] ..
  *              offsets[e + 1] of A and C (as clearmoe_dispatch leaves them, on

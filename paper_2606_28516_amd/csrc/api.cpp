@@ -1655,10 +1655,13 @@ int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, cons
     if (!byte_format(p.a_format) || !byte_format(p.b_format)) return CLEARMOE_ERR_UNSUPPORTED;
     if (!bytes && p.out != CLEARMOE_F32 && p.out != CLEARMOE_BF16) return CLEARMOE_ERR_UNSUPPORTED;
     if (p.M < 0 || p.M >= (int64_t{1} << 31) || p.N < 1 || p.N > kMaxDim || p.K < 16 || p.K > kMaxDim ||
-        p.K % 16 != 0 || p.M > (int64_t{1} << 44) / p.N)
+        p.K % 16 != 0)
         return CLEARMOE_ERR_INVALID_ARG;
     if (p.groups < 0 || p.groups > 64 || (p.gelu != 0 && p.gelu != 1) || p.reserved != 0)
         return CLEARMOE_ERR_INVALID_ARG;
+    const int out = p.out == CLEARMOE_F32 ? kQ8OutF32 : p.out == CLEARMOE_BF16 ? kQ8OutBf16
+                    : p.out == CLEARMOE_E4M3 ? kQ8OutE4M3 : kQ8OutE5M2;
+    if (!q8_launch_fits(p.M, p.N, p.groups, out)) return CLEARMOE_ERR_INVALID_ARG;
     const int64_t cols = bytes ? q8_cols(p.N) : p.N;
     const int64_t lda = p.lda != 0 ? p.lda : p.K, ldc = p.ldc != 0 ? p.ldc : cols;
     if (lda < p.K || lda > kMaxStride || lda % 16 != 0) return CLEARMOE_ERR_INVALID_ARG;
@@ -1678,8 +1681,7 @@ int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, cons
     g.bias = bias;
     g.C = c; g.ldc = ldc;
     g.SC = static_cast<uint8_t*>(c_scale); g.sc_ld = q8_scale_cols(p.N);
-    g.out = p.out == CLEARMOE_F32 ? kQ8OutF32 : p.out == CLEARMOE_BF16 ? kQ8OutBf16
-            : p.out == CLEARMOE_E4M3 ? kQ8OutE4M3 : kQ8OutE5M2;
+    g.out = out;
     g.gelu = p.gelu;
     g.fa = p.a_format - CLEARMOE_E4M3; g.fb = p.b_format - CLEARMOE_E4M3;
     g.wide = aligned(c, 16) && ldc % piece_elems(p.out) == 0 && p.N % piece_elems(p.out) == 0;

@@ -916,6 +916,12 @@ constexpr int64_t kQ8FewLds = 48 << 10;
 
 }  // namespace
 
+bool q8_launch_fits(int64_t M, int N, int groups, int out) {
+    // 256 x 128 tiles take whatever is large, over 512 threads for float32
+    // results and 256 for others (the grid is rounded up to whole XCDs)
+    const int64_t threads = out == kQ8OutF32 ? 512 : 256;
+    return ((M + 255) / 256 + groups) * q8_blocks(N) <= (int64_t{1} << 32) / threads - kGbXcds;
+}
 bool q8_few_supported(int64_t M, int64_t K) {
     const int64_t rows = M < 16 ? M : 16;
     return M <= kQ8FewRows && rows * (q8_blocks(K) * (kQ8Block + 1) + 16) <= kQ8FewLds;

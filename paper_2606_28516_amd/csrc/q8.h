@@ -117,6 +117,9 @@ struct Q8Desc {
     int seg_merge;               // always 0 (the tile search's field)
 };
 hipError_t launch_gemm_q8(const Q8Desc& g, hipStream_t st);
+// Whether the product fits one launch: a grid holds less than 2^32 threads,
+// and one that asks for more is cut without an error.
+bool q8_launch_fits(int64_t M, int N, int groups, int out);
 
 // The same product in e4m3 for a few rows of A that are still float32
 // (a_f32) or bfloat16 [M, K0] (row stride K0, K = q8_cols(K0)): every workgroup

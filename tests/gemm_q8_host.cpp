@@ -23,9 +23,36 @@ static void row_tiles() {
                 expect(gb_row_tiles(static_cast<int>(rows), bm) == (rows + bm - 1) / bm, "row tiles", rows, bm);
 }
 
+// No product is taken whose launch, by any of the kernels, passes 2^32 threads.
+static void launch() {
+    const int64_t top = (int64_t{1} << 31) - 1;
+    expect(q8_launch_fits(top, 1, 64, kQ8OutBf16), "rows", top, kQ8OutBf16);
+    expect(!q8_launch_fits(top, 1, 0, kQ8OutF32), "rows", top, kQ8OutF32);
+    expect(q8_launch_fits(top - 256 * 8, 128, 0, kQ8OutF32), "rows", top - 256 * 8, kQ8OutF32);
+    expect(!q8_launch_fits(top - 256 * 8, 128, 1, kQ8OutF32), "rows of a group", top - 256 * 8, kQ8OutF32);
+    expect(!q8_launch_fits(top, 129, 0, kQ8OutBf16), "columns", 129, kQ8OutBf16);
+    expect(!q8_launch_fits(int64_t{1} << 28, 65536, 0, kQ8OutE4M3), "columns", 65536, kQ8OutE4M3);
+    for (int out : {kQ8OutF32, kQ8OutBf16, kQ8OutE4M3, kQ8OutE5M2})
+        for (int groups : {0, 1, 64})
+            for (int N : {1, 128, 129, 1000, 65536}) {
+                // the most rows that are taken
+                int64_t lo = 0, hi = top;
+                while (lo < hi) {
+                    const int64_t mid = lo + (hi - lo + 1) / 2;
+                    if (q8_launch_fits(mid, N, groups, out)) lo = mid;
+                    else hi = mid - 1;
+                }
+                const int64_t tiles = ((lo + 255) / 256 + groups) * ((N + 127) / 128);
+                const int64_t threads = (tiles + 7) / 8 * 8 * (out == kQ8OutF32 ? 512 : 256);
+                expect(threads < (int64_t{1} << 32), "threads of a launch", lo, N);
+                expect(lo == top || threads > (int64_t{1} << 32) - (int64_t{1} << 20) * 512, "refused too early", lo, N);
+            }
+}
+
 int main(int argc, char** argv) {
     if (argc < 2) return 2;
     if (std::strcmp(argv[1], "row_tiles") == 0) row_tiles();
+    else if (std::strcmp(argv[1], "launch") == 0) launch();
     else return 2;
     return g_bad != 0;
 }

@@ -65,3 +65,19 @@ def test_a_group_of_almost_2_31_rows(last):
     del a, sa, out
     torch.cuda.empty_cache()
     assert right == (M - last, last)
+
+
+def test_most_rows_of_a_float32_result():
+    """The largest launch of the 512-thread tiles that is taken."""
+    M, N, K = 2 ** 31 - 2048, 1, 16
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB of device memory")
+    a = torch.full((M, K), 0x38, dtype=torch.uint8, device="cuda").view(E4M3)
+    sa = torch.full((M, 4), 127, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+    b, sb = a[:1].clone(), sa[:1].clone()
+    out = torch.full((M, N), 7.5, dtype=torch.float32, device="cuda")
+    cm.quantized_gemm(a, sa, b, sb, out_dtype=torch.float32, out=out)
+    right = int((out == 16).sum())
+    del a, sa, out
+    torch.cuda.empty_cache()
+    assert right == M

@@ -305,8 +305,10 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
     // logits of (token, expert) and how far they may be off: a wave adds up
     // the products of its steps and then the waves' sums are added, each
     // addition off by 2^-23 of the magnitudes' sum at most (the instructions
-    // may truncate), itself off as little
+    // may truncate), itself off as little; and what of a product or an addition
+    // lies below the normal numbers may be lost, from the magnitudes too
     const float slack = static_cast<float>(STEP * (steps / kFewWaves + 2) + 2 * kFewWaves) * (0x1p-23f * 1.01f);
+    const float lost = static_cast<float>(2 * STEP * steps + 4 * kFewWaves) * 0x1p-126f;
     if (!a.routed)
         for (int p = tid; p < nt * 16 * EG; p += kFewThreads) {
             const int t = p / (16 * EG), e = p % (16 * EG);
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
             const uint32_t u = __float_as_uint(l + 0.0f);
             s_key[t][e] = e >= E || l != l ? 0u : (u & 0x80000000u) != 0 ? ~u : u | 0x80000000u;
             s_lf[0][t][e] = e < E ? l : 0.0f;
-            s_lf[1][t][e] = e < E ? (m + fabsf(b)) * slack : -__builtin_inff();
+            s_lf[1][t][e] = e < E ? (m + fabsf(b)) * slack + lost : -__builtin_inff();
         }
     __syncthreads();
     if (!a.routed) {

@@ -228,6 +228,28 @@ def _queue(x: torch.Tensor, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
+def _empty(x: torch.Tensor, shape: tuple, dtype, stream, kept: bool = True) -> torch.Tensor:
+    """A new tensor on x's device for a call on `stream` (None: the current
+    one).  Its memory comes from that stream's own pool, so that nothing still
+    queued elsewhere uses it and what is freed on return goes to later work of
+    the same stream only.  kept: the caller gets it, and may let go of it while
+    the current stream still reads it."""
+    if stream is None:
+        return x.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        t = x.new_empty(shape, dtype=dtype)
+    if kept and t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
+def _workspace(n: int, x: torch.Tensor, stream, what: str = "shape") -> torch.Tensor:
+    """n bytes for the duration of a call on `stream`."""
+    if n == 0:
+        raise ClearMoEError(f"invalid {what}")
+    return _empty(x, (n,), torch.uint8, stream, kept=False)
+
+
 def make_shape(T, D, E, k, dtype, H=0, r=0, q=0, renorm=1) -> Shape:
     """renorm = 1: the top-k gates renormalised over the selected experts;
     0: their probabilities under the softmax over all E."""
@@ -250,9 +272,9 @@ def route(x, Wg, bg, k: int, ws: Optional[torch.Tensor] = None, stream=None, ren
     T, D = x.shape
     E = Wg.shape[0]
     s = make_shape(T, D, E, k, _dt(x), renorm=renorm)
-    ws = alloc_workspace(s, x.device) if ws is None else ws
-    idx = torch.empty((T, k), dtype=torch.int32, device=x.device)
-    gate = torch.empty((T, k), dtype=torch.float32, device=x.device)
+    ws = _workspace(workspace_bytes(s), x, stream) if ws is None else ws
+    idx = _empty(x, (T, k), torch.int32, stream)
+    gate = _empty(x, (T, k), torch.float32, stream)
     rc = lib().clearmoe_route(ctypes.byref(s), _p(x), _p(Wg), _p(bg), _p(idx), _p(gate), _p(ws),
                               ws.numel(), _stream(stream))
     _check(rc, "clearmoe_route")
@@ -275,9 +297,9 @@ def route_ex(x, router: Router, E: int, k: int, ws: Optional[torch.Tensor] = Non
     """clearmoe_route_ex: returns (idx [T,k] int32, -1 = empty slot; gate [T,k])."""
     T, D = x.shape
     s = make_shape(T, D, E, k, _dt(x), renorm=renorm)
-    ws = alloc_workspace(s, x.device) if ws is None else ws
-    idx = torch.empty((T, k), dtype=torch.int32, device=x.device)
-    gate = torch.empty((T, k), dtype=torch.float32, device=x.device)
+    ws = _workspace(workspace_bytes(s), x, stream) if ws is None else ws
+    idx = _empty(x, (T, k), torch.int32, stream)
+    gate = _empty(x, (T, k), torch.float32, stream)
     rc = lib().clearmoe_route_ex(ctypes.byref(s), ctypes.byref(router), _p(x), _p(idx), _p(gate),
                                  _p(ws), ws.numel(), _stream(stream))
     _check(rc, "clearmoe_route_ex")
@@ -293,13 +315,12 @@ def dispatch(idx, E: int, ws: Optional[torch.Tensor] = None, x=None, D: Optional
     else:
         D, dtype = 8, BF16          # no rows to copy: D only has to be valid
     s = make_shape(T, D, E, k, dtype)
-    ws = alloc_workspace(s, idx.device) if ws is None else ws
-    dev = idx.device
-    counts = torch.empty(E, dtype=torch.int32, device=dev)
-    offsets = torch.empty(E + 1, dtype=torch.int32, device=dev)
-    perm = torch.empty(T * k, dtype=torch.int32, device=dev)
-    inv = torch.empty(T * k, dtype=torch.int32, device=dev)
-    xperm = None if x is None else torch.empty((T * k, D), dtype=x.dtype, device=dev)
+    ws = _workspace(workspace_bytes(s), idx, stream) if ws is None else ws
+    counts = _empty(idx, (E,), torch.int32, stream)
+    offsets = _empty(idx, (E + 1,), torch.int32, stream)
+    perm = _empty(idx, (T * k,), torch.int32, stream)
+    inv = _empty(idx, (T * k,), torch.int32, stream)
+    xperm = None if x is None else _empty(idx, (T * k, D), x.dtype, stream)
     rc = lib().clearmoe_dispatch(ctypes.byref(s), _p(idx), _p(ws), ws.numel(), _p(counts),
                                  _p(offsets), _p(perm), _p(inv), _p(x), _p(xperm),
                                  DISPATCH_HIST_IN_WS if hist_in_ws else 0, _stream(stream))
@@ -313,7 +334,7 @@ def combine(ye, inv, gate, out: Optional[torch.Tensor] = None, stream=None):
     D = ye.shape[1]
     E = max(k, 1)
     s = make_shape(T, D, E, k, _dt(ye))
-    y = torch.empty((T, D), dtype=ye.dtype, device=ye.device) if out is None else out
+    y = _empty(ye, (T, D), ye.dtype, stream) if out is None else out
     rc = lib().clearmoe_combine(ctypes.byref(s), _p(ye), _p(inv), _p(gate), _p(y),
                                 _stream(stream))
     _check(rc, "clearmoe_combine")
@@ -331,12 +352,8 @@ def _layer_call(name, ws_bytes, x, W1, b1, US, Vt, b2, P, Q, Wg, bg, k, ws, out,
     r = US.shape[1]
     E, _, q = P.shape
     s = make_shape(T, D, E, k, _dt(x), H=H, r=r, q=q, renorm=renorm)
-    if ws is None:
-        n = ws_bytes(s)
-        if n == 0:
-            raise ClearMoEError("invalid shape")
-        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
-    y = torch.empty((T, D), dtype=x.dtype, device=x.device) if out is None else out
+    ws = _workspace(ws_bytes(s), x, stream) if ws is None else ws
+    y = _empty(x, (T, D), x.dtype, stream) if out is None else out
     rc = getattr(lib(), name)(ctypes.byref(s), _p(x), _p(W1), _p(b1), _p(US), _p(Vt), _p(b2),
                               _p(P), _p(Q), _p(Wg), _p(bg), _p(y), _p(idx_out), _p(gate_out),
                               _p(ws), ws.numel(), _stream(stream))
@@ -362,7 +379,7 @@ def ffn_forward_noalloc(x, W1, b1, US, Vt, b2, P, Q, Wg, bg, k: int,
     r = US.shape[1]
     E, _, q = P.shape
     s = make_shape(T, D, E, k, _dt(x), H=H, r=r, q=q, renorm=renorm)
-    y = torch.empty((T, D), dtype=x.dtype, device=x.device) if out is None else out
+    y = _empty(x, (T, D), x.dtype, stream) if out is None else out
     rc = lib().clearmoe_ffn_forward_noalloc(ctypes.byref(s), _p(x), _p(W1), _p(b1), _p(US), _p(Vt),
                                             _p(b2), _p(P), _p(Q), _p(Wg), _p(bg), _p(y),
                                             _p(idx_out), _p(gate_out), _stream(stream))
@@ -388,8 +405,8 @@ def ffn_forward_ex(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
     r = US.shape[1]
     E, _, q = P.shape
     s = make_shape(T, D, E, k, _dt(x), H=H, r=r, q=q, renorm=renorm)
-    ws = alloc_workspace(s, x.device) if ws is None else ws
-    y = torch.empty((T, D), dtype=x.dtype, device=x.device) if out is None else out
+    ws = _workspace(workspace_bytes(s), x, stream) if ws is None else ws
+    y = _empty(x, (T, D), x.dtype, stream) if out is None else out
     rc = lib().clearmoe_ffn_forward_ex(ctypes.byref(s), ctypes.byref(router), _p(x), _p(W1),
                                        _p(b1), _p(US), _p(Vt), _p(b2), _p(P), _p(Q), _p(y),
                                        _p(idx_out), _p(gate_out), _p(ws), ws.numel(),
@@ -404,8 +421,8 @@ def dense_ffn_forward(x, W1, b1, W2, b2, ws: Optional[torch.Tensor] = None,
     T, D = x.shape
     H = W1.shape[0]
     s = make_shape(T, D, 1, 1, _dt(x), H=H)
-    ws = alloc_workspace(s, x.device) if ws is None else ws
-    y = torch.empty((T, D), dtype=x.dtype, device=x.device) if out is None else out
+    ws = _workspace(workspace_bytes(s), x, stream) if ws is None else ws
+    y = _empty(x, (T, D), x.dtype, stream) if out is None else out
     rc = lib().clearmoe_dense_ffn_forward(ctypes.byref(s), _p(x), _p(W1), _p(b1), _p(W2), _p(b2),
                                           _p(y), _p(ws), ws.numel(), _stream(stream))
     _check(rc, "clearmoe_dense_ffn_forward")
@@ -441,11 +458,8 @@ def stack_forward(x, layers, H: int, E: int, r: int, q: int, residual: bool = Tr
     s = stack_shape(x, H, E, r, q)
     arr = (StackLayer * len(layers))(*layers)
     if ws is None:
-        n = int(lib().clearmoe_stack_workspace_bytes(ctypes.byref(s), arr, len(layers)))
-        if n == 0:
-            raise ClearMoEError("invalid stack")
-        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
-    y = torch.empty_like(x) if out is None else out
+        ws = _workspace(int(lib().clearmoe_stack_workspace_bytes(ctypes.byref(s), arr, len(layers))), x, stream, "stack")
+    y = _empty(x, tuple(x.shape), x.dtype, stream) if out is None else out
     rc = lib().clearmoe_stack_forward(ctypes.byref(s), arr, len(layers), 1 if residual else 0,
                                       _p(x), _p(y), _p(ws), ws.numel(), _stream(stream))
     _check(rc, "clearmoe_stack_forward")
@@ -475,7 +489,7 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
     H, r, (E, _, q), dt = W1.shape[0], US.shape[1], P.shape, x.dtype
     s = Shape(T, D, H, E, k, r, q, _dt(x), renorm)
     f32 = torch.float32
-    y = torch.empty_like(x) if out is None else out
+    y = out if out is not None else torch.empty_like(x) if stream is None else _empty(x, (T, D), dt, stream)
     # (one expression: a check a tensor would cost a small call 2 us)
     if not (W1.dtype is US.dtype is Vt.dtype is P.dtype is Q.dtype is y.dtype is dt and W1.shape == (H, D)
             and US.shape == (D, r) and Vt.shape == (r, H) and P.shape == (E, D, q) and Q.shape == (E, q, H)
@@ -485,7 +499,7 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
             and (gate_out is None or (gate_out.numel() == T * k and gate_out.dtype is f32))):
         raise ClearMoEError(f"the tensors do not fit x [{T}, {D}] {dt}, W1 [{H}, .], US [., {r}] and P [{E}, ., {q}]")
     xp, st = _ptr(x), _queue(x, stream)
-    ws = alloc_few_workspace(s, x.device) if ws is None else ws
+    ws = _workspace(few_workspace_bytes(s), x, stream) if ws is None else ws
     rc = lib().clearmoe_ffn_forward_few(ctypes.byref(s), ctypes.byref(router), xp, _ptr(W1),
                                         _ptr(b1), _ptr(US), _ptr(Vt), _ptr(b2), _ptr(P), _ptr(Q), _ptr(y),
                                         _ptr(idx_out), _ptr(gate_out), _ptr(ws), ws.numel(), st)
@@ -534,8 +548,8 @@ def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
     st = _queue(x, stream)
     dt, code = _dt(x), _format(fmt)
     nr = rows if block_rows == 1 else -(-rows // 128)
-    v = x.new_empty((*lead, rows, _value_cols(cols)), dtype=fmt)
-    s = x.new_empty((*lead, nr, _scale_cols(cols)), dtype=torch.float8_e8m0fnu)
+    v = _empty(x, (*lead, rows, _value_cols(cols)), fmt, stream)
+    s = _empty(x, (*lead, nr, _scale_cols(cols)), torch.float8_e8m0fnu, stream)
     rc = lib().clearmoe_quantize(dt, code, block_rows, batch, rows, cols, x.data_ptr(), ldx, v.data_ptr(),
                                  s.data_ptr(), st)
     _check(rc, "clearmoe_quantize")
@@ -565,8 +579,8 @@ def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offset
             _shaped_or_none(bias, torch.float32, (*lead, N), "bias"),
             _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets"))
     st = _queue(a, stream)
-    c = a.new_empty((M, cols), dtype=out_dtype) if out is None else out
-    cs = a.new_empty((M, _scale_cols(N)), dtype=e8) if byte else None
+    c = _empty(a, (M, cols), out_dtype, stream) if out is None else out
+    cs = _empty(a, (M, _scale_cols(N)), e8, stream) if byte else None
     rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), *args, _shaped(c, out_dtype, (M, cols), "out"), _ptr(cs), st)
     _check(rc, "clearmoe_quantized_gemm")
     return (c, cs) if byte else c
@@ -600,8 +614,8 @@ def quantized_ffn_forward(x, W1, W1_scale, b1, W2, W2_scale, b2, offsets=None,
             _shaped_or_none(b2, f32, (*lead, D), "b2"),
             _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets"))
     xp, st = _ptr(x), _queue(x, stream)
-    ws = alloc_quantized_workspace(s, x.device) if ws is None else ws
-    y = torch.empty_like(x) if out is None else out
+    ws = _workspace(quantized_workspace_bytes(s), x, stream) if ws is None else ws
+    y = _empty(x, (T, D), x.dtype, stream) if out is None else out
     rc = lib().clearmoe_quantized_ffn_forward(ctypes.byref(s), xp, *args, _shaped(y, x.dtype, (T, D), "out"),
                                               _ptr(ws), ws.numel(), st)
     _check(rc, "clearmoe_quantized_ffn_forward")

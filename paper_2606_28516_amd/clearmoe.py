@@ -192,40 +192,43 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(s.cuda_stream)
 
 
-def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
-    """_p as a plain address: ctypes turns it into the pointer argument."""
+def _ptr(t: Optional[torch.Tensor], dev: int) -> Optional[int]:
+    """The address of a tensor on device dev (_p with a check of the device;
+    ctypes turns it into the pointer argument)."""
     if t is None:
         return None
-    if not t.is_cuda:
-        raise ClearMoEError("tensor is not on the GPU")
+    if t.get_device() != dev:
+        raise ClearMoEError("the tensors are not on one device" if t.is_cuda else "tensor is not on the GPU")
     if not t.is_contiguous():
         raise ClearMoEError("tensor is not contiguous")
     return t.data_ptr()
 
 
-def _shaped(t: torch.Tensor, dtype, shape: tuple, what: str) -> int:
+def _shaped(t: torch.Tensor, dtype, shape: tuple, what: str, dev: int) -> int:
     """The address of a tensor that has to have this type and shape."""
-    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
     if t.dtype is not dtype or t.shape != shape:
         raise ClearMoEError(f"{what} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
+    return _ptr(t, dev)
 
 
-def _shaped_or_none(t: Optional[torch.Tensor], dtype, shape: tuple, what: str) -> Optional[int]:
-    return None if t is None else _shaped(t, dtype, shape, what)
+def _shaped_or_none(t: Optional[torch.Tensor], dtype, shape: tuple, what: str, dev: int) -> Optional[int]:
+    return None if t is None else _shaped(t, dtype, shape, what, dev)
 
 
-def _queue(x: torch.Tensor, stream) -> int:
-    """The stream of a call on x's device, which has to be the current one: the
-    kernels are launched there.  The current stream is asked for by its handle
-    (a torch.cuda.Stream object costs 3 us, a quarter of a small call)."""
-    dev = x.get_device()
+def _queue(dev: int, stream) -> int:
+    """The stream of a call on tensors of device dev, which has to be the
+    current one: the kernels are launched there.  The current stream is asked
+    for by its handle (a torch.cuda.Stream object costs 3 us, a quarter of a
+    small call)."""
+    if dev < 0:
+        raise ClearMoEError("tensor is not on the GPU")
     if dev != torch._C._cuda_getDevice():
         raise ClearMoEError("the tensors are not on the current device")
-    if stream is not None:
-        return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(dev)
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ClearMoEError("the stream is not of the tensors' device")
+    return stream.cuda_stream
 
 
 def _empty(x: torch.Tensor, shape: tuple, dtype, stream, kept: bool = True) -> torch.Tensor:
@@ -498,11 +501,13 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
             and (idx_out is None or (idx_out.numel() == T * k and idx_out.dtype is torch.int32))
             and (gate_out is None or (gate_out.numel() == T * k and gate_out.dtype is f32))):
         raise ClearMoEError(f"the tensors do not fit x [{T}, {D}] {dt}, W1 [{H}, .], US [., {r}] and P [{E}, ., {q}]")
-    xp, st = _ptr(x), _queue(x, stream)
+    dev = x.get_device()
+    st = _queue(dev, stream)
     ws = _workspace(few_workspace_bytes(s), x, stream) if ws is None else ws
-    rc = lib().clearmoe_ffn_forward_few(ctypes.byref(s), ctypes.byref(router), xp, _ptr(W1),
-                                        _ptr(b1), _ptr(US), _ptr(Vt), _ptr(b2), _ptr(P), _ptr(Q), _ptr(y),
-                                        _ptr(idx_out), _ptr(gate_out), _ptr(ws), ws.numel(), st)
+    rc = lib().clearmoe_ffn_forward_few(ctypes.byref(s), ctypes.byref(router), _ptr(x, dev), _ptr(W1, dev),
+                                        _ptr(b1, dev), _ptr(US, dev), _ptr(Vt, dev), _ptr(b2, dev), _ptr(P, dev),
+                                        _ptr(Q, dev), _ptr(y, dev), _ptr(idx_out, dev), _ptr(gate_out, dev),
+                                        _ptr(ws, dev), ws.numel(), st)
     _check(rc, "clearmoe_ffn_forward_few")
     return y
 
@@ -534,8 +539,6 @@ def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
     blocks up to a multiple of 4] in float8_e8m0fnu)."""
     if x.dim() not in (2, 3):
         raise ClearMoEError("quantize takes [rows, cols] or [batch, rows, cols]")
-    if not x.is_cuda:
-        raise ClearMoEError("tensor is not on the GPU")
     lead = x.shape[:-2]
     batch = x.shape[0] if lead else 1
     rows, cols = x.shape[-2:]
@@ -545,7 +548,7 @@ def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
         ldx = x.stride(-2) if rows > 1 else x.stride(0) if batch > 1 else cols
         if x.numel() > 0 and ((cols > 1 and x.stride(-1) != 1) or (batch > 1 and x.stride(0) != rows * ldx)):
             raise ClearMoEError("rows must be contiguous and evenly spaced over the batch")
-    st = _queue(x, stream)
+    st = _queue(x.get_device(), stream)
     dt, code = _dt(x), _format(fmt)
     nr = rows if block_rows == 1 else -(-rows // 128)
     v = _empty(x, (*lead, rows, _value_cols(cols)), fmt, stream)
@@ -574,14 +577,16 @@ def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offset
         raise ClearMoEError(f"unsupported dtype {out_dtype}")
     cols, sc, e8 = _value_cols(N) if byte else N, _scale_cols(K), torch.float8_e8m0fnu
     p = Product(M, N, K, E, _format(a.dtype), _format(b.dtype), _OUTS[out_dtype], 1 if gelu else 0, 0, 0, 0)
-    args = (_ptr(a), _shaped(a_scale, e8, (M, sc), "a_scale"), _ptr(b),
-            _shaped(b_scale, e8, (*lead, -(-N // 128), sc), "b_scale"),
-            _shaped_or_none(bias, torch.float32, (*lead, N), "bias"),
-            _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets"))
-    st = _queue(a, stream)
+    dev = a.get_device()
+    args = (_ptr(a, dev), _shaped(a_scale, e8, (M, sc), "a_scale", dev), _ptr(b, dev),
+            _shaped(b_scale, e8, (*lead, -(-N // 128), sc), "b_scale", dev),
+            _shaped_or_none(bias, torch.float32, (*lead, N), "bias", dev),
+            _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets", dev))
+    st = _queue(dev, stream)
     c = _empty(a, (M, cols), out_dtype, stream) if out is None else out
     cs = _empty(a, (M, _scale_cols(N)), e8, stream) if byte else None
-    rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), *args, _shaped(c, out_dtype, (M, cols), "out"), _ptr(cs), st)
+    rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), *args, _shaped(c, out_dtype, (M, cols), "out", dev),
+                                       _ptr(cs, dev), st)
     _check(rc, "clearmoe_quantized_gemm")
     return (c, cs) if byte else c
 
@@ -606,18 +611,19 @@ def quantized_ffn_forward(x, W1, W1_scale, b1, W2, W2_scale, b2, offsets=None,
     E, H = (lead[0] if lead else 1), W1.shape[-2]
     e4, e8, f32 = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float32
     s = Shape(T, D, H, E, 1, 0, 0, _dt(x), 1)
-    args = (_shaped(W1, e4, (*lead, H, _value_cols(D)), "weights W1"),
-            _shaped(W1_scale, e8, (*lead, -(-H // 128), _scale_cols(D)), "W1_scale"),
-            _shaped_or_none(b1, f32, (*lead, H), "b1"),
-            _shaped(W2, e4, (*lead, D, _value_cols(H)), "weights W2"),
-            _shaped(W2_scale, e8, (*lead, -(-D // 128), _scale_cols(H)), "W2_scale"),
-            _shaped_or_none(b2, f32, (*lead, D), "b2"),
-            _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets"))
-    xp, st = _ptr(x), _queue(x, stream)
+    dev = x.get_device()
+    args = (_shaped(W1, e4, (*lead, H, _value_cols(D)), "weights W1", dev),
+            _shaped(W1_scale, e8, (*lead, -(-H // 128), _scale_cols(D)), "W1_scale", dev),
+            _shaped_or_none(b1, f32, (*lead, H), "b1", dev),
+            _shaped(W2, e4, (*lead, D, _value_cols(H)), "weights W2", dev),
+            _shaped(W2_scale, e8, (*lead, -(-D // 128), _scale_cols(H)), "W2_scale", dev),
+            _shaped_or_none(b2, f32, (*lead, D), "b2", dev),
+            _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets", dev))
+    xp, st = _ptr(x, dev), _queue(dev, stream)
     ws = _workspace(quantized_workspace_bytes(s), x, stream) if ws is None else ws
     y = _empty(x, (T, D), x.dtype, stream) if out is None else out
-    rc = lib().clearmoe_quantized_ffn_forward(ctypes.byref(s), xp, *args, _shaped(y, x.dtype, (T, D), "out"),
-                                              _ptr(ws), ws.numel(), st)
+    rc = lib().clearmoe_quantized_ffn_forward(ctypes.byref(s), xp, *args, _shaped(y, x.dtype, (T, D), "out", dev),
+                                              _ptr(ws, dev), ws.numel(), st)
     _check(rc, "clearmoe_quantized_ffn_forward")
     return y
 

@@ -891,24 +891,37 @@ int64_t q8_tiles(const Q8Desc& g, int bm, int bn) {
 //             256 x 128                                38.3         108
 //   8 bits    64 x 128         7.2  6.0   9.6   6.2    25.1 11.9     89   35
 //             256 x 128 (duo) 12.8  9.6  13.4  10.0    20.5 11.0     57   25
+Q8Kernel q8_choose(const Q8Desc& g) {
+    // bytes: two workgroups of 64 x 128 on every CU, or more rows a workgroup
+    if (g.out == kQ8OutE4M3 || g.out == kQ8OutE5M2) return q8_tiles(g, 64, 128) <= 512 ? kQ8Small : kQ8Large;
+    if (g.out == kQ8OutF32)
+        return q8_tiles(g, 16, 16) <= 800 ? kQ8Rows : q8_tiles(g, 64, 64) <= 1024 ? kQ8Small : kQ8Large;
+    return q8_tiles(g, 16, 16) <= 400     ? kQ8Rows
+           : q8_tiles(g, 64, 64) <= 640   ? kQ8Small
+           : q8_tiles(g, 256, 128) < 192  ? kQ8Middle
+                                          : kQ8Large;
+}
+
+template <int FA, int FB, int OUT>
+hipError_t q8_launch(const Q8Desc& g, hipStream_t st) {
+    const Q8Kernel kernel = q8_choose(g);
+    if constexpr (OUT == kQ8OutE4M3 || OUT == kQ8OutE5M2) {
+        return kernel == kQ8Small ? q8_tile<1, 2, 2, 1, 2, 2, FA, FB, OUT>(g, st) : q8_duo<FA, FB, OUT>(g, st);
+    } else {
+        if (kernel == kQ8Rows) return q8_rows<FA, FB, OUT == kQ8OutF32>(g, st);
+        if (kernel == kQ8Small) return q8_tile<2, 2, 2, 1, 1, 2, FA, FB, OUT>(g, st);
+        if constexpr (OUT == kQ8OutF32) return q8_tile<1, 4, 2, 2, 2, 2, FA, FB, OUT>(g, st);
+        else
+            return kernel == kQ8Middle ? q8_tile<1, 4, 2, 1, 2, 4, FA, FB, OUT>(g, st) : q8_duo<FA, FB, OUT>(g, st);
+    }
+}
+
 template <int FA, int FB>
 hipError_t q8_formats(const Q8Desc& g, hipStream_t st) {
-    if (g.out == kQ8OutE4M3 || g.out == kQ8OutE5M2) {
-        // two workgroups of 64 x 128 on every CU, or more rows a workgroup
-        const bool few = q8_tiles(g, 64, 128) <= 512;
-        if (g.out == kQ8OutE4M3)
-            return few ? q8_tile<1, 2, 2, 1, 2, 2, FA, FB, kQ8OutE4M3>(g, st) : q8_duo<FA, FB, kQ8OutE4M3>(g, st);
-        return few ? q8_tile<1, 2, 2, 1, 2, 2, FA, FB, kQ8OutE5M2>(g, st) : q8_duo<FA, FB, kQ8OutE5M2>(g, st);
-    }
-    if (g.out == kQ8OutF32) {
-        if (q8_tiles(g, 16, 16) <= 800) return q8_rows<FA, FB, true>(g, st);
-        if (q8_tiles(g, 64, 64) <= 1024) return q8_tile<2, 2, 2, 1, 1, 2, FA, FB, kQ8OutF32>(g, st);
-        return q8_tile<1, 4, 2, 2, 2, 2, FA, FB, kQ8OutF32>(g, st);
-    }
-    if (q8_tiles(g, 16, 16) <= 400) return q8_rows<FA, FB, false>(g, st);
-    if (q8_tiles(g, 64, 64) <= 640) return q8_tile<2, 2, 2, 1, 1, 2, FA, FB, kQ8OutBf16>(g, st);
-    if (q8_tiles(g, 256, 128) < 192) return q8_tile<1, 4, 2, 1, 2, 4, FA, FB, kQ8OutBf16>(g, st);
-    return q8_duo<FA, FB, kQ8OutBf16>(g, st);
+    if (g.out == kQ8OutE4M3) return q8_launch<FA, FB, kQ8OutE4M3>(g, st);
+    if (g.out == kQ8OutE5M2) return q8_launch<FA, FB, kQ8OutE5M2>(g, st);
+    if (g.out == kQ8OutF32) return q8_launch<FA, FB, kQ8OutF32>(g, st);
+    return q8_launch<FA, FB, kQ8OutBf16>(g, st);
 }
 
 // The LDS that the quantised form of a few rows may take.
@@ -916,6 +929,7 @@ constexpr int64_t kQ8FewLds = 48 << 10;
 
 }  // namespace
 
+Q8Kernel q8_kernel(const Q8Desc& g) { return q8_choose(g); }
 bool q8_launch_fits(int64_t M, int N, int groups, int out) {
     // 256 x 128 tiles take whatever is large, over 512 threads for float32
     // results and 256 for others (the grid is rounded up to whole XCDs)

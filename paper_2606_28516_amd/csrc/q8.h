@@ -117,6 +117,10 @@ struct Q8Desc {
     int seg_merge;               // always 0 (the tile search's field)
 };
 hipError_t launch_gemm_q8(const Q8Desc& g, hipStream_t st);
+// The kernel that a product takes: 16 x 16 tiles, 64 x 64 (bytes: 64 x 128),
+// 128 x 128 or 256 x 128.
+enum Q8Kernel { kQ8Rows, kQ8Small, kQ8Middle, kQ8Large };
+Q8Kernel q8_kernel(const Q8Desc& g);
 // Whether the product fits one launch: a grid holds less than 2^32 threads,
 // and one that asks for more is cut without an error.
 bool q8_launch_fits(int64_t M, int N, int groups, int out);

@@ -2,6 +2,7 @@
 // test_gemm_q8_host.py.  Prints each violation; exits with 1 if any.
 #include <cstdint>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 
 #include "gemm_tile.h"
@@ -49,10 +50,26 @@ static void launch() {
             }
 }
 
+// The kernel of each product M N groups out (as q8.h numbers them).
+static void kernels(int n, char** v) {
+    static int32_t offsets[65];
+    const char* names[] = {"rows", "small", "middle", "large"};
+    for (int i = 0; i + 3 < n; i += 4) {
+        Q8Desc g{};
+        g.M = std::atol(v[i]);
+        g.N = std::atoi(v[i + 1]);
+        g.nseg = std::atoi(v[i + 2]);
+        g.seg_offsets = g.nseg > 0 ? offsets : nullptr;
+        g.out = std::atoi(v[i + 3]);
+        std::printf("%s\n", names[q8_kernel(g)]);
+    }
+}
+
 int main(int argc, char** argv) {
     if (argc < 2) return 2;
     if (std::strcmp(argv[1], "row_tiles") == 0) row_tiles();
     else if (std::strcmp(argv[1], "launch") == 0) launch();
+    else if (std::strcmp(argv[1], "kernels") == 0) kernels(argc - 2, argv + 2);
     else return 2;
     return g_bad != 0;
 }

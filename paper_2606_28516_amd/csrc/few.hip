@@ -128,18 +128,33 @@ __device__ __forceinline__ void few_logits(const FewArgs& a, const T* x, int wav
         if (lane == 0) lg[e] = s + (a.bg != nullptr ? static_cast<double>(a.bg[e]) : 0.0);
     }
 }
-// Rank of expert e among lg[0 .. E): by logit descending, ties to the lower
-// index, NaN last.
-template <typename F>
-__device__ __forceinline__ int few_rank(const F* lg, int E, int e) {
-    const F l = lg[e];
+// The k experts of logits lg[0 .. E) (LDS) into idx, by logit descending, ties
+// to the lower index; all threads call it, barriers before and after are the
+// caller's.  With NaN among them the routers' rule decides: one pick after the
+// other, each from the first expert that is left on, which only a larger logit
+// replaces.
+__device__ __forceinline__ void few_choose(const double* lg, int E, int k, int tid, int32_t* idx) {
+    if (tid >= E) return;
+    const double l = lg[tid];
     int rank = 0;
+    bool nan = false;
     for (int o = 0; o < E; ++o) {
-        const F m = lg[o];
-        const bool tie = m == l || (m != m && l != l);
-        rank += m > l || (l != l && m == m) || (tie && o < e);
+        const double m = lg[o];
+        rank += m > l || (m == l && o < tid);
+        nan = nan || m != m;
     }
-    return rank;
+    if (!nan) {
+        if (rank < k) idx[rank] = tid;
+    } else if (tid == 0) {
+        uint64_t taken = 0;
+        for (int j = 0; j < k; ++j) {
+            int best = -1;
+            for (int e = 0; e < E; ++e)
+                if ((taken >> e & 1u) == 0 && (best < 0 || lg[e] > lg[best])) best = e;
+            taken |= 1ull << best;
+            idx[j] = best;
+        }
+    }
 }
 
 // Routing of token t for the caller and the second kernel: choice and gates by
@@ -149,10 +164,7 @@ __device__ __forceinline__ void few_route(const FewArgs& a, int t, double* lg, d
     const int tid = threadIdx.x, E = a.E, k = a.k;
     few_logits<T, MODE>(a, static_cast<const T*>(a.x) + static_cast<int64_t>(t) * a.D, tid >> 6, tid & 63, lg);
     __syncthreads();
-    if (tid < E) {
-        const int rank = few_rank(lg, E, tid);
-        if (rank < k) idx[rank] = tid;
-    }
+    few_choose(lg, E, k, tid, idx);
     __syncthreads();
     if (tid < E) ex[tid] = exp(lg[tid] - lg[idx[0]]);
     __syncthreads();
@@ -364,13 +376,9 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
             const int t = __builtin_ctz(left);
             few_logits<T, MODE>(a, x + static_cast<int64_t>(t) * D, wave, lane, s_lg);
             __syncthreads();
-            if (tid < E) {
-                const int rank = few_rank(s_lg, E, tid);
-                if (rank < k) {
-                    s_idx[t][rank] = tid;
-                    atomicOr(&s_used, 1ull << tid);
-                }
-            }
+            few_choose(s_lg, E, k, tid, s_idx[t]);
+            __syncthreads();
+            if (tid < k) atomicOr(&s_used, 1ull << s_idx[t][tid]);
             __syncthreads();
         }
     } else {

@@ -1,5 +1,5 @@
 """The few-token layer's experts where float32 logits say least: sums of
-products below its range, operands below it, products above it.  Every
+products below its range, operands below it, products above it, NaN.  Every
 workgroup chooses for itself; the outputs have to be those of the routing that
 is given out."""
 import pytest
@@ -65,3 +65,40 @@ def test_products_above_the_range(T, D, E, dtype):
     L["Wg"][0, 5] = 2.0 ** 100
     L["Wg"][2, 3], L["Wg"][2, 40], L["Wg"][2, 5] = 2.0 ** 70, -2.0 ** 70, 2.0 ** 101
     _check(L, 2)
+
+
+def _same(a, b, atol):
+    return bool(((a - b).abs() <= atol).logical_or(a.isnan() & b.isnan()).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("adaptive,renorm", [(False, 0), (False, 1), (True, 0), (True, 1)])
+@pytest.mark.parametrize("E,k,experts", [(6, 2, (0,)), (6, 2, (0, 1)), (6, 2, (1, 3, 5)), (6, 2, (2,)),
+                                         (6, 2, (0, 1, 2, 3, 4, 5)), (20, 2, (0, 19)), (7, 2, (6,))])
+def test_nan_logits_are_chosen_as_by_the_router(E, k, experts, adaptive, renorm, dtype):
+    """NaN in some experts' router rows: route_ex's choice and gates."""
+    L = _layer(16, 64, 96, E, k, 16, 8, dtype, 3)
+    for e in experts:
+        L["Wg"][e, 0] = float("nan")
+    rt = _router(L, adaptive=adaptive, tau=0.6 if adaptive else 0.0)
+    _, idx, gate = _few(L, rt, renorm)
+    want, wgate = cm.route_ex(L["x"], rt, E, k, renorm=renorm)
+    assert torch.equal(idx, want)
+    assert _same(gate, wgate, 2e-5)       # route_ex's gates may come from float32 logits
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k", [1, 3, 6])
+def test_nan_and_infinite_logits_of_some_tokens(k, dtype):
+    """An infinite activation makes infinite logits, and NaN where the router's
+    weight is zero; the other tokens stay as they were."""
+    L = _layer(16, 64, 96, 6, k, 16, 8, dtype, 3)
+    L["Wg"][0, 3] = L["Wg"][4, 3] = 0
+    rt = _router(L)
+    y0, i0, g0 = _few(L, rt)
+    L["x"][2, 3], L["x"][3, 3], L["x"][9] = float("inf"), -float("inf"), float("nan")
+    y, idx, gate = _few(L, rt)
+    want, wgate = cm.route_ex(L["x"], rt, 6, k)
+    assert torch.equal(idx, want) and _same(gate, wgate, 2e-5)
+    keep = [t for t in range(16) if t not in (2, 3, 9)]
+    assert torch.equal(y[keep], y0[keep]) and torch.equal(gate[keep], g0[keep])

@@ -341,7 +341,6 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
     static_assert(RB >= 32 && 64 % CH == 0 && 32 % RPI == 0, "whole rows per store");
     const int lrow = lane & 31, lh = lane >> 5;
     const int cols = static_cast<int>(q8_cols(g.N));
-    const bool cut = cols != g.N;                // the last 16 bytes of a row hold bytes past N
     if (g.gelu)
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -351,6 +350,17 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
                 for (int v = 0; v < 16; ++v) acc[i][j][v] = F32 ? gelu_erf(acc[i][j][v]) : q8_gelu(acc[i][j][v]);
     float mx[TM];
     if constexpr (!F32 && !BF16) {
+        // Bytes past N are zeros whatever the row holds (their sums are zeros
+        // times A: NaN where A is no number or infinite); 16 of them at most
+        // are stored.
+        if (cols != g.N && nw + 32 * TN > g.N)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (nw + j * 32 + 16 * (v >> 3) + 8 * lh + (v & 7) >= g.N)
+#pragma unroll
+                        for (int i = 0; i < TM; ++i) acc[i][j][v] = 0.0f;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             // a lane and the one 32 further hold a row's columns; infinities
@@ -459,18 +469,8 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
                 }
             } else {
                 const int n = nw + ch * 16;
-                if (n >= cols) continue;
-                u32x4 o = w;
-                if (cut && n + 16 > g.N) {
-                    // bytes past N are zeros whatever the row holds (their sums
-                    // are zeros times A, NaN where A is no number or infinite)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int keep = g.N - n - 4 * q;
-                        o[q] = keep >= 4 ? w[q] : keep <= 0 ? 0u : w[q] & ((1u << (8 * keep)) - 1u);
-                    }
-                }
-                *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(g.C) + (t.m_lo + rl) * g.ldc + n) = o;
+                if (n < cols)
+                    *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(g.C) + (t.m_lo + rl) * g.ldc + n) = w;
             }
         }
         __builtin_amdgcn_wave_barrier();

@@ -206,6 +206,8 @@ def _ptr(t: Optional[torch.Tensor], dev: int) -> Optional[int]:
 
 def _shaped(t: torch.Tensor, dtype, shape: tuple, what: str, dev: int) -> int:
     """The address of a tensor that has to have this type and shape."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype is not dtype or t.shape != shape:
         raise ClearMoEError(f"{what} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
     return _ptr(t, dev)
@@ -621,7 +623,7 @@ def quantized_ffn_forward(x, W1, W1_scale, b1, W2, W2_scale, b2, offsets=None,
             _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets", dev))
     xp, st = _ptr(x, dev), _queue(dev, stream)
     ws = _workspace(quantized_workspace_bytes(s), x, stream) if ws is None else ws
-    y = _empty(x, (T, D), x.dtype, stream) if out is None else out
+    y = out if out is not None else torch.empty_like(x) if stream is None else _empty(x, (T, D), x.dtype, stream)
     rc = lib().clearmoe_quantized_ffn_forward(ctypes.byref(s), xp, *args, _shaped(y, x.dtype, (T, D), "out", dev),
                                               _ptr(ws, dev), ws.numel(), st)
     _check(rc, "clearmoe_quantized_ffn_forward")

@@ -312,19 +312,24 @@ int clearmoe_dense_ffn_forward(const clearmoe_shape* shape, const void* x, const
 
 /* ---- The layer for a few tokens --------------------------------------------
  * clearmoe_ffn_forward_ex for at most CLEARMOE_FEW_MAX_TOKENS tokens: the same
- * arguments, layouts and results up to rounding (z, t and u keep float32's
- * accuracy here, where the other entry points round them to dtype), as two
- * kernels whose time hardly depends on the token count: the form for serving
- * single tokens and small batches.
+ * arguments, layouts and results up to rounding, as two kernels: the form for
+ * serving single tokens and small batches.  All sums are float32; in bfloat16,
+ * z is held to 16 bits, t and u in float32, where the other entry points round
+ * all three to bfloat16.  Sixteen tokens share a read of the weights: a
+ * 768 -> 3072 top-2 layer takes 14 us for 1 token, 19 for 16, 34 for 64
+ * (clearmoe_ffn_forward_ex: 43, 47, 51).
  *   - Any router but one with class tokens (dense_stride > 0:
  *     CLEARMOE_ERR_UNSUPPORTED).  Linear routers run inside the first kernel:
  *     gates from logits in double, and the experts that those choose; an MLP
- *     router runs before it, as clearmoe_route_ex.
- *   - Any D, H, r, q (r + k q <= 12288, else CLEARMOE_ERR_UNSUPPORTED); where
- *     all are multiples of 8 (bf16) or 4 (float32) and every tensor is 16-byte
- *     aligned, memory is read in 16-byte pieces, else element by element, for
- *     which element alignment is enough (an MLP router's weights keep the
- *     alignment clearmoe_route_ex asks for).
+ *     router runs before it, as clearmoe_route_ex (its launches and its time,
+ *     about 30 us, are added).
+ *   - Any D, H, r, q (r + k q <= 12288, else CLEARMOE_ERR_UNSUPPORTED).
+ *     Element alignment is enough for every tensor, except that with an MLP
+ *     router x and the router's weights keep the alignment clearmoe_route_ex
+ *     asks for.  Where D, H, r and q are multiples of 8 (bf16) or 4 (float32)
+ *     and every tensor is 16-byte aligned, memory is read in aligned 16-byte
+ *     pieces; else in 16-byte pieces from any element on, and row ends of less
+ *     than a piece element by element.
  *   - More tokens: CLEARMOE_ERR_TOO_LARGE.
  * The workspace holds clearmoe_few_workspace_bytes(shape) bytes, 256-byte
  * aligned.  The kernels are timed as the stages CLEARMOE_STAGE_FC1 and
@@ -368,8 +373,16 @@ int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int6
                       hipStream_t stream);
 
 /* A product C = epi(A B^T + bias) of quantised matrices, A [M, K] with row
- * scales and B [N, K] with 128 x 128 scales, summed in float32 from the first
- * to the last block.
+ * scales and B [N, K] with 128 x 128 scales.  The sums are float32; how much of
+ * a product enters them depends on the result:
+ *   F32    all of it;
+ *   BF16, bytes   the 8-bit matrix instructions (twice as fast) add eight
+ *          products that follow each other along k after cutting each 14 bits
+ *          below the largest of them: on normal data 1.5e-5 of the result's
+ *          norm, at worst 2^-10 of the magnitudes' sum.  Where large products
+ *          cancel, take F32 results.
+ * Which blocks are added first depends on the sizes alone: the same call gives
+ * the same result every time.
  *   M, N, K    0 <= M < 2^31; N, K in 1 .. 65536, K a multiple of 16 (the width
  *              of the value rows: zeros past the columns add nothing); what one
  *              launch holds: (ceil(M / 256) + groups) ceil(N / 128) at most
@@ -377,13 +390,15 @@ int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int6
  *   groups     0: one B.  E (1 .. 64): B [E, N, K], scales [E, ceil(N / 128), .]
  *              and bias [E, N], one for each expert; rows offsets[e] ..
  *              offsets[e + 1] of A and C (as clearmoe_dispatch leaves them, on
- *              the device) belong to expert e.  Offsets are clamped to
- *              [0, M]; rows of C outside all groups are left as they were.
+ *              the device, ascending) belong to expert e.  Offsets are clamped
+ *              to [0, M]; rows of C and c_scale outside all groups are left as
+ *              they were.
  *   a_format, b_format   CLEARMOE_E4M3 or CLEARMOE_E5M2, in any combination.
  *   out        CLEARMOE_F32 or CLEARMOE_BF16: C [M, N], rounded once; or a byte
  *              format: C is quantised as clearmoe_quantize with block_rows 1
  *              would (from float32), values in C and scales in c_scale.
- *   gelu       1: GELU after the bias.
+ *   gelu       1: GELU after the bias (NaN of an infinite sum).  BF16 and byte
+ *              results: from values within 3.3e-6 of themselves (6e-9 below -6).
  *   lda, ldc   row strides in elements; 0: K, and N (byte formats:
  *              round_up(N, 16)).  lda and a byte format's ldc are multiples
  *              of 16; both at most 2^22.
@@ -407,7 +422,8 @@ int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, cons
 /* The dense FFN, or the caller's own experts' FFN between clearmoe_dispatch
  * (with rows) and clearmoe_combine, in e4m3:
  *     y = Q8(GELU(Q8(x) W1^T + b1)) W2^T + b2,
- * Q8 quantising rows in blocks of 128 columns.  x, y [T, D] (dtype); W1 [H, D],
+ * Q8 quantising rows in blocks of 128 columns, the products those of
+ * clearmoe_quantized_gemm (the first to bytes).  x, y [T, D] (dtype); W1 [H, D],
  * W2 [D, H] quantised in e4m3 with 128 x 128 scales; biases float32 or NULL.
  * With offsets [E + 1] (device), weights are [E, H, .] and [E, D, .], biases
  * [E, H] and [E, D], and row p uses expert e with offsets[e] <= p <

@@ -489,7 +489,8 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
                     ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                     idx_out=None, gate_out=None, stream=None, renorm: int = 1):
     """clearmoe_ffn_forward_few: the whole layer for at most FEW_MAX_TOKENS
-    tokens, with any router without class tokens.  Returns y."""
+    tokens, with any router without class tokens (its tensors on x's device).
+    Returns y."""
     T, D = x.shape
     H, r, (E, _, q), dt = W1.shape[0], US.shape[1], P.shape, x.dtype
     s = Shape(T, D, H, E, k, r, q, _dt(x), renorm)
@@ -566,8 +567,11 @@ def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offset
     """clearmoe_quantized_gemm: a [M, K] with 1 x 128 scales times b [N, K] with
     128 x 128 scales, as quantize returns them, or, with offsets [E + 1], times
     b [E, N, K] for the rows of each expert (rows outside all groups are left
-    as out had them).  Returns C [M, N] in out_dtype; for an 8-bit out_dtype
-    (values [M, N up to a multiple of 16], scales)."""
+    as out had them; their scales, of an 8-bit result, are not set).  Returns C
+    [M, N] in out_dtype; for an 8-bit out_dtype (values [M, N up to a multiple
+    of 16], scales).  Sums of a float32 result hold every product; those of the
+    others come from the 8-bit matrix instructions, which cut eight products at
+    a time 14 bits below the largest."""
     M, K = a.shape
     E = 0 if offsets is None else b.shape[0]
     lead = (E,) if E else ()

@@ -18,9 +18,13 @@
 // Both kernels wait for memory (us on an MI355X under a profiler, where an
 // empty kernel takes 2.3 to 2.8; the bytes alone 0.4 to 2.2 for both):
 //                                                  hidden    out
-//   1 token, 384 -> 1536, E = 8, k = 1, bfloat16     6.4     5.2
-//   1 token, 768 -> 3072, E = 8, k = 2, bfloat16     8.2     6.4
-//   16 tokens of these, adaptive router             12.5     7.4
+//   1 token, 384 -> 1536, E = 8, k = 1, bfloat16     6.6     5.2
+//   1 token, 768 -> 3072, E = 8, k = 2, bfloat16     8.2     5.3 to 6.4
+//   16 tokens of these, adaptive router             12.6     7.6
+// More tokens choose more experts: a wave has six 16-row tiles of Vt and Q
+// where one token gives it three, which is most of what the first kernel grows
+// by.  (Both experts of a token count, also where the adaptive router drops
+// the second.)
 // Slices of 16 or 64 hidden units, 256 or 1024 threads and the logits in double
 // on the matrix instructions (2.2 us more) were slower.
 #include "few.h"
@@ -298,8 +302,9 @@ __global__ __launch_bounds__(kFewThreads) void k_few_hidden(FewArgs a, int route
     }
     __syncthreads();
     // z: the waves' sums, bias, GELU.  In bfloat16 z is kept as two parts, the
-    // rounded value and what the rounding left, and both are multiplied: twice
-    // the (idle) matrix instructions, and t and u keep float32's accuracy.
+    // rounded value and what the rounding left (rounded too: 16 bits in all),
+    // and both are multiplied: twice the (idle) matrix instructions, and t and u
+    // are off by 2^-16 of z at most beside float32's sums.
 #pragma unroll
     for (int i = 0; i < ZN; ++i) {
         const int t = (i * kFewThreads + tid) / HS, c = (i * kFewThreads + tid) % HS;

@@ -143,7 +143,7 @@ hipError_t q8_rows(const Q8Desc& g, hipStream_t st) {
 // into LDS (rows of `pitch` bytes, then rows of nk scale bytes), then as
 // k_q8_rows.  The first blocks of B are on their way meanwhile, so a call is
 // two trips to memory at most, which is what bounds it: 1 x 3072 x 768 takes
-// 4.5 us under a profiler and 1 x 768 x 3072 4.8, where an empty kernel takes
+// 4.4 us under a profiler and 1 x 768 x 3072 5.1, where an empty kernel takes
 // 2.3 to 2.8 and the weights' bytes 0.5.
 template <typename TA, typename TC>
 __global__ __launch_bounds__(512) void k_q8_few(Q8Desc g, const TA* A, int K0, int mtiles, int ntiles, int pitch) {
@@ -480,12 +480,13 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
 // 256 x 128 tile over four waves (64 x 128 each), two workgroups on a CU, so
 // that one's epilogue runs beside the other's matrix instructions.  80 KB of
 // LDS each: A has two stage buffers, B one, which is free as soon as its
-// fragments are in registers.  Measured on an MI355X: 50432 x 768 x 3072 to
-// bfloat16 128 us (1865 TFLOP/s), 50432 x 3072 x 768 with GELU to e4m3 163 to
-// 196 us, 8192 x 8192 x 8192 482 us (2283 TFLOP/s; the library's large 8-bit
-// product: 3065).  With few stages (k = 384, 768) the epilogue's vector work
-// and stores bound it; over many, LDS does: 192 KB of fragments and 96 KB of
-// new bytes a stage and CU take longer than its 2048 cycles of instructions.
+// fragments are in registers.  Measured on an MI355X, calls in a row (and under
+// a profiler, the first ones): 50432 x 768 x 3072 to bfloat16 118 us (142),
+// 2020 TFLOP/s, 50432 x 3072 x 768 with GELU to e4m3 157 (198), 8192 x 8192 x
+// 8192 440 (482), 2500 TFLOP/s; the library's large 8-bit product: 3065.  With
+// few stages (k = 384, 768) the epilogue's vector work and stores bound it;
+// over many, LDS does: 192 KB of fragments and 96 KB of new bytes a stage and
+// CU take longer than its 2048 cycles of instructions.
 // 256 x 256 tiles over eight waves, a grid that stays on the chip and takes
 // tile after tile, and fetching B earlier were no faster.
 template <int FA, int FB, int OUT>
@@ -634,7 +635,9 @@ void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group) {
 // that is alone on its CU waits for one stage after the other, with two groups
 // for half as many (512 x 768 x 3072, 64 x 64 tiles: one group 10.3 us, two
 // 8.6, four 8.8; float32 17.6, 13.1, 12.5; more stages ahead change nothing).
-// WIDE: float32 results, on bfloat16 instructions (see above).
+// WIDE: float32 results, on bfloat16 instructions (see above): eight a stage
+// that wait for each other, their operands widened just before, which is what
+// float32 takes longer here.
 template <int KG, int WM, int WN, int TM, int TN, int NS, int FA, int FB, int OUT>
 __global__ __launch_bounds__(64 * KG * WM * WN) void k_q8_tile(Q8Desc g, int mtiles, int ntiles, int group) {
     constexpr bool WIDE = OUT == kQ8OutF32;

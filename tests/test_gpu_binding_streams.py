@@ -63,3 +63,51 @@ def test_a_call_on_a_busy_stream(make, T):
         assert torch.equal(y, want)
         torch.cuda.synchronize()
         del y, other, busy
+
+
+def test_a_forked_stream_of_a_capture():
+    """Two calls side by side in one captured graph, one of them on a stream
+    that joins the capture, without workspaces of the caller's."""
+    x, W1, b1, W2, b2 = _ffn_inputs(40, 192, 768, 0, BF16, 3)
+    w1, s1 = cm.quantize(W1.cuda(), block_rows=128)
+    w2, s2 = cm.quantize(W2.cuda(), block_rows=128)
+    x, b1, b2 = x.cuda(), b1.cuda(), b2.cuda()
+    call = lambda **kw: cm.quantized_ffn_forward(x, w1, s1, b1, w2, s2, b2, **kw)
+    side, stream, graph = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    call(), call(stream=side)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        side.wait_stream(stream)
+        there, here = call(stream=side), call()
+        values, _ = cm.quantize(x, stream=side)
+        stream.wait_stream(side)
+        both = there + here
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for _ in range(4):
+        x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+        want, bytes_ = call(), cm.quantize(x)[0].view(torch.uint8)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(there, want) and torch.equal(here, want) and torch.equal(both, want + want)
+        assert torch.equal(values.view(torch.uint8), bytes_)
+
+
+def test_an_mlp_router_captured():
+    L = _layer(9, 384, 520, 8, 2, 64, 16, BF16, 1, mlp=64)
+    rt = _router(L)
+    ws = cm.alloc_few_workspace(cm.make_shape(9, 384, 8, 2, cm.BF16, H=520, r=64, q=16))
+    call = lambda: cm.ffn_forward_few(L["x"], L["W1"], L["b1"], L["US"], L["Vt"], L["b2"], L["P"], L["Q"], rt, 2, ws=ws)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    call()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        got = call()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    for _ in range(4):
+        L["x"].copy_(torch.randn(9, 384, device="cuda", generator=g))
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)

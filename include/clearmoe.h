@@ -356,10 +356,22 @@ int clearmoe_ffn_forward_few(const clearmoe_shape* shape, const clearmoe_router*
  * dividing by them is exact and the matrix instructions apply them. */
 typedef enum { CLEARMOE_E4M3 = 2, CLEARMOE_E5M2 = 3 } clearmoe_byte_format;
 
+/* ---- 4-bit floating point with block scales ----------------------------------
+ * CLEARMOE_E2M1 in the place of a format: OCP e2m1, the values 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 and their negatives (codes 0 .. 7, and 8 more), with a scale for
+ * each block of 32 columns of a row (microscaled 4-bit floating point):
+ *   values  rows of 16 ceil(cols / 32) bytes, the even column of a byte in its
+ *           low half, zeros past cols;
+ *   scales  as above, in rows of round_up(ceil(cols / 32), 4) bytes.
+ * Blocks are 1 x 32 for activations and weights alike.  The format has neither
+ * NaN nor infinity: a block that would hold one has the scale 255 (NaN) and the
+ * values 0, and all of it reads as NaN. */
+enum { CLEARMOE_E2M1 = 5 };
+
 /* x [batch, rows, cols] (dtype CLEARMOE_F32 or CLEARMOE_BF16; rows ldx >= cols
  * elements apart, batches rows * ldx) to values [batch, rows, .] and scales
  * [batch, ceil(rows / block_rows), .] of a format; block_rows is 1
- * (activations) or 128 (weights).  A block's scale is the smallest power of
+ * (activations; CLEARMOE_E2M1: all) or 128 (weights).  A block's scale is the smallest power of
  * two, at least 2^-126, for which its largest finite magnitude stays within
  * the format's range (1 for a block of zeros); every value is then rounded
  * once, to nearest even.  NaN stays NaN, and so does infinity in e4m3; in e5m2
@@ -371,6 +383,47 @@ typedef enum { CLEARMOE_E4M3 = 2, CLEARMOE_E5M2 = 3 } clearmoe_byte_format;
 int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int64_t rows,
                       int32_t cols, const void* x, int64_t ldx, void* values, void* scales,
                       hipStream_t stream);
+
+/* Back: y [batch, rows, cols] (dtype; rows ldy >= cols elements apart, batches
+ * rows * ldy), each value times its scale, exactly in float32 and rounded once
+ * to bfloat16 (exactly but below 2^-126).  A scale of 255 gives NaN; what
+ * passes the type's range is infinite.  Arguments as clearmoe_quantize; y needs
+ * element alignment. */
+int clearmoe_dequantize(int format, int block_rows, int64_t batch, int64_t rows, int32_t cols,
+                        const void* values, const void* scales, int dtype, void* y, int64_t ldy,
+                        hipStream_t stream);
+
+/* The root-mean-square norm ahead of such a product, with the residual's
+ * addition:
+ *     h = x + residual,   y = h (mean(h^2) + eps)^(-1/2) weight   by rows,
+ * h rounded to dtype (the stream that goes on), y computed from the rounded h in
+ * float32 with the sum of squares in double, and rounded once.
+ *   dtype      CLEARMOE_F32 or CLEARMOE_BF16: x, residual and sum.
+ *   out        dtype, or CLEARMOE_E4M3 or CLEARMOE_E5M2: y is quantised as
+ *              clearmoe_quantize with block_rows 1 would (from float32), values
+ *              in y and scales in y_scale.
+ *   rows, cols 0 <= rows < 2^31, 1 <= cols <= 65536.
+ *   ldx, ldr, lds, ldy   row strides of x, residual, sum and y in elements, at
+ *              most 2^31; 0: cols (byte formats' ldy: round_up(cols, 16), and a
+ *              multiple of 16).
+ *   eps        a normal float32 > 0 (a row of zeros gives zeros).
+ * residual may be NULL (h = x), weight [cols] too (ones), and sum, which gets h
+ * (it may be x or residual itself, and y, of dtype, any of the three that is
+ * not sum; no other overlap).  NaN and infinite values give what the formula
+ * does: NaN makes its row NaN, an infinity NaN at its place and zeros at the
+ * finite ones.  Element alignment is enough for float tensors; byte results
+ * are 16-byte aligned, their scales 4-byte. */
+typedef struct {
+    int64_t rows;
+    int32_t cols;
+    int32_t dtype;
+    int32_t out;
+    float eps;
+    int64_t ldx, ldr, lds, ldy;
+} clearmoe_norm;
+
+int clearmoe_rms_norm(const clearmoe_norm* norm, const void* x, const void* residual,
+                      const float* weight, void* y, void* y_scale, void* sum, hipStream_t stream);
 
 /* A product C = epi(A B^T + bias) of quantised matrices, A [M, K] with row
  * scales and B [N, K] with 128 x 128 scales.  The sums are float32; how much of
@@ -403,7 +456,17 @@ int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int6
  *              round_up(N, 16)).  lda and a byte format's ldc are multiples
  *              of 16; both at most 2^22.
  * a, b and byte results are 16-byte aligned, scales 4-byte, F32 and BF16
- * results element-aligned. */
+ * results element-aligned.
+ *
+ * 4-bit B (b_format CLEARMOE_E2M1): [N, K] or [E, N, K] with a scale for each 32
+ * values of a row, so b_scale is [N, .] or [E, N, .].
+ *   a_format   CLEARMOE_E4M3, or CLEARMOE_E2M1: then K, lda are multiples of 32,
+ *              and products run at twice the rate.  (With e4m3 rows of a K that
+ *              is no multiple of 32, b's rows are padded further than a's.)
+ *   out        CLEARMOE_F32, CLEARMOE_BF16, CLEARMOE_E4M3, or CLEARMOE_E2M1: C
+ *              is quantised to 4 bits, ldc a multiple of 32.
+ *   sums       of 4-bit A hold all of a product; of e4m3 A as above (1.2e-5 of
+ *              the result's norm is cut but for F32 results). */
 typedef struct {
     int64_t M;
     int32_t N, K;
@@ -440,6 +503,17 @@ int clearmoe_quantized_ffn_forward(const clearmoe_shape* shape, const void* x, c
                                    const void* W1_scale, const float* b1, const void* W2,
                                    const void* W2_scale, const float* b2, const int32_t* offsets,
                                    void* y, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The same with the formats of the activations (what Q8 above rounds x and z
+ * to) and of the weights: CLEARMOE_E4M3 and CLEARMOE_E4M3, or weights in
+ * CLEARMOE_E2M1 ([H, D] and [D, H] with scales of 1 x 32) and activations in
+ * CLEARMOE_E4M3 or CLEARMOE_E2M1; else CLEARMOE_ERR_UNSUPPORTED.  The same
+ * workspace serves all of them. */
+int clearmoe_quantized_ffn_forward_ex(const clearmoe_shape* shape, int activations, int weights,
+                                      const void* x, const void* W1, const void* W1_scale,
+                                      const float* b1, const void* W2, const void* W2_scale,
+                                      const float* b2, const int32_t* offsets, void* y, void* ws,
+                                      size_t ws_bytes, hipStream_t stream);
 
 /* ---- Stage timing (measurement support) -----------------------------------
  * Kernel stages of the entry points above.  While timing is on, the kernel of

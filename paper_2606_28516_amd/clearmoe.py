@@ -23,7 +23,7 @@ __all__ = ["ClearMoEError", "Shape", "lib", "version", "workspace_bytes", "alloc
            "stack_forward", "Router", "make_router", "route_ex",
            "ffn_forward_ex", "FEW_MAX_TOKENS", "few_workspace_bytes", "alloc_few_workspace",
            "ffn_forward_few", "Product", "quantize", "quantized_gemm", "quantized_workspace_bytes",
-           "alloc_quantized_workspace", "quantized_ffn_forward"]
+           "alloc_quantized_workspace", "quantized_ffn_forward", "Norm", "dequantize", "rms_norm"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libclearmoe.so")
@@ -37,7 +37,8 @@ SYMBOLS = ("clearmoe_version", "clearmoe_source_digest", "clearmoe_status_string
            "clearmoe_ffn_forward_noalloc", "clearmoe_stack_workspace_bytes",
            "clearmoe_stack_forward", "clearmoe_few_workspace_bytes", "clearmoe_ffn_forward_few",
            "clearmoe_quantize", "clearmoe_quantized_gemm", "clearmoe_quantized_workspace_bytes",
-           "clearmoe_quantized_ffn_forward")
+           "clearmoe_quantized_ffn_forward", "clearmoe_quantized_ffn_forward_ex", "clearmoe_dequantize",
+           "clearmoe_rms_norm")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 ERR_TOO_LARGE = 5
 FEW_MAX_TOKENS = 64
@@ -67,6 +68,13 @@ class Product(ctypes.Structure):
                 ("a_format", ctypes.c_int32), ("b_format", ctypes.c_int32), ("out", ctypes.c_int32),
                 ("gelu", ctypes.c_int32), ("reserved", ctypes.c_int32), ("lda", ctypes.c_int64),
                 ("ldc", ctypes.c_int64)]
+
+
+class Norm(ctypes.Structure):
+    """clearmoe_norm: the root-mean-square norm of rows."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("out", ctypes.c_int32), ("eps", ctypes.c_float), ("ldx", ctypes.c_int64), ("ldr", ctypes.c_int64),
+                ("lds", ctypes.c_int64), ("ldy", ctypes.c_int64)]
 
 
 class StackLayer(ctypes.Structure):
@@ -146,6 +154,13 @@ def lib():
         L.clearmoe_quantized_workspace_bytes.argtypes = [sp]
         L.clearmoe_quantized_ffn_forward.restype = ctypes.c_int
         L.clearmoe_quantized_ffn_forward.argtypes = [sp] + [vp] * 10 + [sz, vp]
+        L.clearmoe_quantized_ffn_forward_ex.restype = ctypes.c_int
+        L.clearmoe_quantized_ffn_forward_ex.argtypes = [sp, ctypes.c_int, ctypes.c_int] + [vp] * 10 + [sz, vp]
+        L.clearmoe_dequantize.restype = ctypes.c_int
+        L.clearmoe_dequantize.argtypes = [ctypes.c_int] * 2 + [ctypes.c_int64] * 2 + [
+            ctypes.c_int32, vp, vp, ctypes.c_int, vp, ctypes.c_int64, vp]
+        L.clearmoe_rms_norm.restype = ctypes.c_int
+        L.clearmoe_rms_norm.argtypes = [ctypes.POINTER(Norm)] + [vp] * 7
         L.clearmoe_stage_name.restype = ctypes.c_char_p
         L.clearmoe_stage_name.argtypes = [ctypes.c_int]
         L.clearmoe_timing_start.restype = ctypes.c_int
@@ -515,23 +530,40 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
     return y
 
 
-# 8-bit formats, and the C ABI's numbers of every output type
+# 8-bit formats, and the C ABI's numbers of every output type; the 4-bit format
+# (two values a byte)
 _FORMATS = {torch.float8_e4m3fn: 2, torch.float8_e5m2: 3}
-_OUTS = {torch.float32: F32, torch.bfloat16: BF16, **_FORMATS}
+_E2M1 = torch.float4_e2m1fn_x2
+_OUTS = {torch.float32: F32, torch.bfloat16: BF16, **_FORMATS, _E2M1: 5}
 
 
 def _format(dtype) -> int:
-    if dtype not in _FORMATS:
-        raise ClearMoEError(f"unsupported 8-bit format {dtype}")
-    return _FORMATS[dtype]
+    if dtype not in _FORMATS and dtype != _E2M1:
+        raise ClearMoEError(f"unsupported 8- or 4-bit format {dtype}")
+    return _OUTS[dtype]
 
 
-def _value_cols(cols: int) -> int:
-    return (cols + 15) // 16 * 16
+def _value_cols(cols: int, fmt=None) -> int:
+    """Elements of a row of values: bytes."""
+    return (cols + 31) // 32 * 16 if fmt is _E2M1 else (cols + 15) // 16 * 16
 
 
-def _scale_cols(cols: int) -> int:
-    return (cols + 511) // 512 * 4
+def _scale_cols(cols: int, fmt=None) -> int:
+    return (cols + 127) // 128 * 4 if fmt is _E2M1 else (cols + 511) // 512 * 4
+
+
+def _row_stride(x, what: str = "rows") -> int:
+    """Elements between the rows of x [..., rows, cols], which may be strided."""
+    if x.is_contiguous():
+        return x.shape[-1]
+    rows, cols = x.shape[-2:]
+    batch = x.shape[0] if x.dim() == 3 else 1
+    ld = x.stride(-2) if rows > 1 else x.stride(0) if batch > 1 else cols
+    if x.numel() > 0 and ((cols > 1 and x.stride(-1) != 1) or (batch > 1 and x.stride(0) != rows * ld)):
+        raise ClearMoEError(f"{what} must be contiguous and evenly spaced over the batch")
+    if ld < cols:
+        raise ClearMoEError(f"{what} must not overlap")
+    return ld
 
 
 def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
@@ -539,27 +571,91 @@ def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
     strided) in 8-bit floating point with a power-of-two scale for each block
     of block_rows (1 or 128) x 128 values.  Returns (values [..., rows, cols up
     to a multiple of 16] in fmt, scales [..., ceil(rows / block_rows), column
-    blocks up to a multiple of 4] in float8_e8m0fnu)."""
+    blocks up to a multiple of 4] in float8_e8m0fnu).
+
+    fmt torch.float4_e2m1fn_x2: 4 bits, blocks of 1 x 32 (block_rows 1), values
+    [..., rows, 16 ceil(cols / 32)] of two each, the even column in the low
+    half; a block with a NaN or infinite value has a NaN scale."""
     if x.dim() not in (2, 3):
         raise ClearMoEError("quantize takes [rows, cols] or [batch, rows, cols]")
     lead = x.shape[:-2]
     batch = x.shape[0] if lead else 1
     rows, cols = x.shape[-2:]
-    if x.is_contiguous():
-        ldx = cols
-    else:
-        ldx = x.stride(-2) if rows > 1 else x.stride(0) if batch > 1 else cols
-        if x.numel() > 0 and ((cols > 1 and x.stride(-1) != 1) or (batch > 1 and x.stride(0) != rows * ldx)):
-            raise ClearMoEError("rows must be contiguous and evenly spaced over the batch")
+    ldx = _row_stride(x)
     st = _queue(x.get_device(), stream)
     dt, code = _dt(x), _format(fmt)
     nr = rows if block_rows == 1 else -(-rows // 128)
-    v = _empty(x, (*lead, rows, _value_cols(cols)), fmt, stream)
-    s = _empty(x, (*lead, nr, _scale_cols(cols)), torch.float8_e8m0fnu, stream)
+    v = _empty(x, (*lead, rows, _value_cols(cols, fmt)), fmt, stream)
+    s = _empty(x, (*lead, nr, _scale_cols(cols, fmt)), torch.float8_e8m0fnu, stream)
     rc = lib().clearmoe_quantize(dt, code, block_rows, batch, rows, cols, x.data_ptr(), ldx, v.data_ptr(),
                                  s.data_ptr(), st)
     _check(rc, "clearmoe_quantize")
     return v, s
+
+
+def dequantize(values, scale, cols: Optional[int] = None, dtype=torch.bfloat16, block_rows: int = 1,
+               out: Optional[torch.Tensor] = None, stream=None):
+    """clearmoe_dequantize: what quantize's result stands for, [..., rows, cols]
+    in float32 or bfloat16 (cols: as x had; default: the values' padded rows)."""
+    if values.dim() not in (2, 3):
+        raise ClearMoEError("dequantize takes [rows, .] or [batch, rows, .]")
+    fmt, lead, rows = values.dtype, values.shape[:-2], values.shape[-2]
+    code, dev = _format(fmt), values.get_device()
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ClearMoEError(f"unsupported dtype {dtype}")
+    if cols is None:
+        cols = values.shape[-1] * (2 if fmt is _E2M1 else 1)
+    nr = rows if block_rows == 1 else -(-rows // 128)
+    args = (_shaped(values, fmt, (*lead, rows, _value_cols(cols, fmt)), "values", dev),
+            _shaped(scale, torch.float8_e8m0fnu, (*lead, nr, _scale_cols(cols, fmt)), "scale", dev))
+    st = _queue(dev, stream)
+    y = _empty(values, (*lead, rows, cols), dtype, stream) if out is None else out
+    if y.dtype != dtype or y.shape != (*lead, rows, cols) or y.get_device() != dev:
+        raise ClearMoEError(f"out must be {dtype} {(*lead, rows, cols)} on the values' device")
+    rc = lib().clearmoe_dequantize(code, block_rows, values.shape[0] if lead else 1, rows, cols, *args, _OUTS[dtype],
+                                   y.data_ptr(), _row_stride(y, "rows of out"), st)
+    _check(rc, "clearmoe_dequantize")
+    return y
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, out_dtype=None,
+             out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None, stream=None):
+    """clearmoe_rms_norm: y = h (mean(h^2) + eps)^(-1/2) weight over the rows of
+    h = x + residual, x [rows, cols] (rows of x, residual, out and sum_out may
+    be strided), weight [cols] float32 or None.  out_dtype: x's (the default),
+    or an 8-bit format: then values and scales as quantize returns them.
+    Returns y, or (values, scales); with a residual or sum_out also h, last (a
+    new tensor, or sum_out, which may be x or residual itself)."""
+    if x.dim() != 2:
+        raise ClearMoEError("rms_norm takes x [rows, cols]")
+    rows, cols = x.shape
+    dt, dev, xt = _dt(x), x.get_device(), x.dtype
+    ot = xt if out_dtype is None else out_dtype
+    byte = ot in _FORMATS
+    if not byte and ot != xt:
+        raise ClearMoEError(f"out_dtype must be {xt} or an 8-bit format, not {ot}")
+    st = _queue(dev, stream)
+    if weight is not None:
+        weight = _shaped(weight, torch.float32, (cols,), "weight", dev)
+    if sum_out is None and residual is not None:
+        sum_out = _empty(x, (rows, cols), xt, stream)
+    yc = _value_cols(cols) if byte else cols
+    y = _empty(x, (rows, yc), ot, stream) if out is None else out
+    for t, what, c, d in ((residual, "residual", cols, xt), (sum_out, "sum_out", cols, xt), (y, "out", yc, ot)):
+        if t is not None and (t.dtype is not d or t.shape != (rows, c) or t.get_device() != dev):
+            raise ClearMoEError(f"{what} must be {d} {(rows, c)} on x's device, not {t.dtype} {tuple(t.shape)}")
+    ys = _empty(x, (rows, _scale_cols(cols)), torch.float8_e8m0fnu, stream) if byte else None
+    p = Norm(rows, cols, dt, _OUTS[ot], eps, _row_stride(x, "rows of x"),
+             0 if residual is None else _row_stride(residual, "rows of residual"),
+             0 if sum_out is None else _row_stride(sum_out, "rows of sum_out"), _row_stride(y, "rows of out"))
+    rc = lib().clearmoe_rms_norm(ctypes.byref(p), x.data_ptr(), None if residual is None else residual.data_ptr(),
+                                 weight, y.data_ptr(), None if ys is None else ys.data_ptr(),
+                                 None if sum_out is None else sum_out.data_ptr(), st)
+    _check(rc, "clearmoe_rms_norm")
+    r = (y, ys) if byte else (y,)
+    if sum_out is not None:
+        r += (sum_out,)
+    return r if len(r) > 1 else y
 
 
 def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offsets=None,
@@ -571,26 +667,36 @@ def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offset
     [M, N] in out_dtype; for an 8-bit out_dtype (values [M, N up to a multiple
     of 16], scales).  Sums of a float32 result hold every product; those of the
     others come from the 8-bit matrix instructions, which cut eight products at
-    a time 14 bits below the largest."""
+    a time 14 bits below the largest.
+
+    b in 4 bits (quantize to torch.float4_e2m1fn_x2: 1 x 32 scales): a in e4m3
+    or in 4 bits too, of as many columns before their padding; out_dtype
+    float32, bfloat16, e4m3 or 4 bits.  Sums of 4-bit a hold every product."""
     M, K = a.shape
     E = 0 if offsets is None else b.shape[0]
     lead = (E,) if E else ()
     N = b.shape[-2]
-    if b.shape != (*lead, N, K):
-        raise ClearMoEError(f"b must be [{'E, ' if E else ''}N, {K}], not {tuple(b.shape)}")
-    byte = out_dtype in _FORMATS
+    four, a4, c4 = b.dtype is _E2M1, a.dtype is _E2M1, out_dtype is _E2M1
+    fa, fb = _format(a.dtype), _format(b.dtype)
+    if a4:
+        K *= 2
+    kb = _value_cols(K, _E2M1) if four else K
+    if b.shape != (*lead, N, kb):
+        raise ClearMoEError(f"b must be [{'E, ' if E else ''}N, {kb}], not {tuple(b.shape)}")
+    byte = out_dtype in _FORMATS or c4
     if out_dtype not in _OUTS:
         raise ClearMoEError(f"unsupported dtype {out_dtype}")
-    cols, sc, e8 = _value_cols(N) if byte else N, _scale_cols(K), torch.float8_e8m0fnu
-    p = Product(M, N, K, E, _format(a.dtype), _format(b.dtype), _OUTS[out_dtype], 1 if gelu else 0, 0, 0, 0)
+    cols, e8 = _value_cols(N, out_dtype) if byte else N, torch.float8_e8m0fnu
+    sbs = (*lead, N, _scale_cols(K, _E2M1)) if four else (*lead, -(-N // 128), _scale_cols(K))
+    p = Product(M, N, K, E, fa, fb, _OUTS[out_dtype], 1 if gelu else 0, 0, 0, 0)
     dev = a.get_device()
-    args = (_ptr(a, dev), _shaped(a_scale, e8, (M, sc), "a_scale", dev), _ptr(b, dev),
-            _shaped(b_scale, e8, (*lead, -(-N // 128), sc), "b_scale", dev),
+    args = (_ptr(a, dev), _shaped(a_scale, e8, (M, _scale_cols(K, a.dtype)), "a_scale", dev), _ptr(b, dev),
+            _shaped(b_scale, e8, sbs, "b_scale", dev),
             _shaped_or_none(bias, torch.float32, (*lead, N), "bias", dev),
             _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets", dev))
     st = _queue(dev, stream)
     c = _empty(a, (M, cols), out_dtype, stream) if out is None else out
-    cs = _empty(a, (M, _scale_cols(N)), e8, stream) if byte else None
+    cs = _empty(a, (M, _scale_cols(N, out_dtype)), e8, stream) if byte else None
     rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), *args, _shaped(c, out_dtype, (M, cols), "out", dev),
                                        _ptr(cs, dev), st)
     _check(rc, "clearmoe_quantized_gemm")
@@ -607,30 +713,36 @@ def alloc_quantized_workspace(shape: Shape, device="cuda") -> torch.Tensor:
 
 def quantized_ffn_forward(x, W1, W1_scale, b1, W2, W2_scale, b2, offsets=None,
                           ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                          stream=None):
-    """clearmoe_quantized_ffn_forward: x [T, D] through an FFN with e4m3 weights
-    (quantize(W, block_rows=128): W1 [H, .], W2 [D, .]), or, with offsets
-    [E + 1], rows sorted by expert through their expert's ([E, H, .],
-    [E, D, .]; rows outside all groups are left as out had them)."""
+                          stream=None, activations=torch.float8_e4m3fn):
+    """clearmoe_quantized_ffn_forward_ex: x [T, D] through an FFN with e4m3
+    weights (quantize(W, block_rows=128): W1 [H, .], W2 [D, .]) or 4-bit ones
+    (quantize(W, torch.float4_e2m1fn_x2)), or, with offsets [E + 1], rows sorted
+    by expert through their expert's ([E, H, .], [E, D, .]; rows outside all
+    groups are left as out had them).  activations: what x and the hidden
+    values are rounded to, e4m3 or, with 4-bit weights, 4 bits too."""
     T, D = x.shape
     lead = () if offsets is None else (W1.shape[0],)
     E, H = (lead[0] if lead else 1), W1.shape[-2]
-    e4, e8, f32 = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float32
+    fmt = _E2M1 if W1.dtype is _E2M1 else torch.float8_e4m3fn
+    e8, f32 = torch.float8_e8m0fnu, torch.float32
+    br = 1 if fmt is _E2M1 else 128              # rows of a scale
     s = Shape(T, D, H, E, 1, 0, 0, _dt(x), 1)
     dev = x.get_device()
-    args = (_shaped(W1, e4, (*lead, H, _value_cols(D)), "weights W1", dev),
-            _shaped(W1_scale, e8, (*lead, -(-H // 128), _scale_cols(D)), "W1_scale", dev),
+    args = (_shaped(W1, fmt, (*lead, H, _value_cols(D, fmt)), "weights W1", dev),
+            _shaped(W1_scale, e8, (*lead, -(-H // br), _scale_cols(D, fmt)), "W1_scale", dev),
             _shaped_or_none(b1, f32, (*lead, H), "b1", dev),
-            _shaped(W2, e4, (*lead, D, _value_cols(H)), "weights W2", dev),
-            _shaped(W2_scale, e8, (*lead, -(-D // 128), _scale_cols(H)), "W2_scale", dev),
+            _shaped(W2, fmt, (*lead, D, _value_cols(H, fmt)), "weights W2", dev),
+            _shaped(W2_scale, e8, (*lead, -(-D // br), _scale_cols(H, fmt)), "W2_scale", dev),
             _shaped_or_none(b2, f32, (*lead, D), "b2", dev),
             _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets", dev))
+    fa = _format(activations)
     xp, st = _ptr(x, dev), _queue(dev, stream)
     ws = _workspace(quantized_workspace_bytes(s), x, stream) if ws is None else ws
     y = out if out is not None else torch.empty_like(x) if stream is None else _empty(x, (T, D), x.dtype, stream)
-    rc = lib().clearmoe_quantized_ffn_forward(ctypes.byref(s), xp, *args, _shaped(y, x.dtype, (T, D), "out", dev),
-                                              _ptr(ws, dev), ws.numel(), st)
-    _check(rc, "clearmoe_quantized_ffn_forward")
+    rc = lib().clearmoe_quantized_ffn_forward_ex(ctypes.byref(s), fa, _OUTS[fmt], xp, *args,
+                                                 _shaped(y, x.dtype, (T, D), "out", dev), _ptr(ws, dev), ws.numel(),
+                                                 st)
+    _check(rc, "clearmoe_quantized_ffn_forward_ex")
     return y
 
 

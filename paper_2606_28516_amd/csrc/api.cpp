@@ -3,6 +3,7 @@
 // the kernel sequence of each entry point on the caller's stream.
 #include "clearmoe.h"
 
+#include <algorithm>
 #include <stdint.h>
 
 #include <mutex>
@@ -1545,7 +1546,7 @@ struct QuantizedLayout {
 bool quantized_few(const clearmoe_shape& s) {
     return q8_few_supported(s.T, q8_cols(s.D)) && q8_few_supported(s.T, q8_cols(s.H));
 }
-QuantizedLayout quantized_layout(const clearmoe_shape& s) {
+QuantizedLayout quantized_layout(const clearmoe_shape& s, bool four) {
     QuantizedLayout L{};
     size_t off = 0;
     auto take = [&](int64_t bytes) {
@@ -1553,10 +1554,10 @@ QuantizedLayout quantized_layout(const clearmoe_shape& s) {
         off += up(static_cast<size_t>(s.T) * static_cast<size_t>(bytes) + 1);
         return at;
     };
-    L.xv = take(q8_cols(s.D));
-    L.xs = take(q8_scale_cols(s.D));
-    L.zv = take(q8_cols(s.H));
-    L.zs = take(q8_scale_cols(s.H));
+    L.xv = take(four ? q4_cols(s.D) : q8_cols(s.D));
+    L.xs = take(four ? q4_scale_cols(s.D) : q8_scale_cols(s.D));
+    L.zv = take(four ? q4_cols(s.H) : q8_cols(s.H));
+    L.zs = take(four ? q4_scale_cols(s.H) : q8_scale_cols(s.H));
     // z in float32 takes the same bytes; a workspace for more rows also holds
     // any number of few ones
     const size_t few = static_cast<size_t>(s.T < kQ8FewRows ? s.T : kQ8FewRows);
@@ -1564,8 +1565,69 @@ QuantizedLayout quantized_layout(const clearmoe_shape& s) {
     L.total = off > z ? off : z;
     return L;
 }
-bool byte_format(int f) { return f == CLEARMOE_E4M3 || f == CLEARMOE_E5M2; }
+// One workspace serves activations in 8 and in 4 bits.
+size_t quantized_bytes(const clearmoe_shape& s) {
+    return std::max(quantized_layout(s, false).total, quantized_layout(s, true).total);
+}
 constexpr int64_t kMaxStride = int64_t{1} << 22;
+bool byte_format(int f) { return f == CLEARMOE_E4M3 || f == CLEARMOE_E5M2; }
+bool float_type(int f) { return f == CLEARMOE_F32 || f == CLEARMOE_BF16; }
+// A format as the kernels number it, and an output type.
+int q8_format(int f) { return f == CLEARMOE_E4M3 ? kQ8E4M3 : f == CLEARMOE_E5M2 ? kQ8E5M2 : kQ8E2M1; }
+int q8_out(int f) {
+    return f == CLEARMOE_F32 ? kQ8OutF32 : f == CLEARMOE_BF16 ? kQ8OutBf16 : f == CLEARMOE_E4M3 ? kQ8OutE4M3
+           : f == CLEARMOE_E5M2 ? kQ8OutE5M2 : kQ8OutE2M1;
+}
+// Quantised matrices of batch x rows x cols in blocks: whether they are at most
+// 2^31 blocks (checked so that no product overflows).
+bool few_blocks(int64_t batch, int64_t rows, int64_t cols, int64_t ld, int format, int block_rows) {
+    constexpr int64_t most = int64_t{1} << 31;
+    if (rows >= most || batch >= most || ld > (int64_t{1} << 40)) return false;
+    const int64_t per = block_rows == 1 ? rows : (rows + kQ8Block - 1) / kQ8Block;
+    const int64_t blocks = format == CLEARMOE_E2M1 ? q4_blocks(cols) : q8_blocks(cols);
+    return batch <= most / per && batch * per <= most / blocks;
+}
+// The product with 4-bit b.
+int quantized_gemm4(const clearmoe_product& p, const void* a, const void* a_scale, const void* b, const void* b_scale,
+                    const float* bias, const int32_t* offsets, void* c, void* c_scale, hipStream_t stream) {
+    const bool a4 = p.a_format == CLEARMOE_E2M1, c4 = p.out == CLEARMOE_E2M1, bytes = c4 || p.out == CLEARMOE_E4M3;
+    if (!a4 && p.a_format != CLEARMOE_E4M3) return CLEARMOE_ERR_UNSUPPORTED;
+    if (!bytes && !float_type(p.out)) return CLEARMOE_ERR_UNSUPPORTED;
+    const int64_t unit = a4 ? kQ4Block : 16;     // values in 16 bytes of a row of a
+    if (p.M < 0 || p.M >= (int64_t{1} << 31) || p.N < 1 || p.N > kMaxDim || p.K < unit || p.K > kMaxDim ||
+        p.K % unit != 0)
+        return CLEARMOE_ERR_INVALID_ARG;
+    if (p.groups < 0 || p.groups > 64 || (p.gelu != 0 && p.gelu != 1) || p.reserved != 0)
+        return CLEARMOE_ERR_INVALID_ARG;
+    const int out = q8_out(p.out);
+    if (!q8_launch_fits(p.M, p.N, p.groups, out)) return CLEARMOE_ERR_INVALID_ARG;
+    const int64_t cols = c4 ? q4_blocks(p.N) * kQ4Block : bytes ? q8_cols(p.N) : p.N;
+    const int64_t lda = p.lda != 0 ? p.lda : p.K, ldc = p.ldc != 0 ? p.ldc : cols;
+    if (lda < p.K || lda > kMaxStride || lda % unit != 0) return CLEARMOE_ERR_INVALID_ARG;
+    if (ldc < cols || ldc > kMaxStride || (bytes && ldc % (c4 ? kQ4Block : 16) != 0)) return CLEARMOE_ERR_INVALID_ARG;
+    if (!b || !b_scale || (p.M > 0 && (!a || !a_scale || !c || (bytes && !c_scale)))) return CLEARMOE_ERR_INVALID_ARG;
+    if ((p.groups > 0) != (offsets != nullptr)) return CLEARMOE_ERR_INVALID_ARG;
+    if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) || !aligned(c_scale, 4) ||
+        !aligned(bias, 4) || !aligned(offsets, 4) || !aligned(c, bytes ? 16 : elem_size(p.out)))
+        return CLEARMOE_ERR_INVALID_ARG;
+    if (p.M == 0) return CLEARMOE_OK;
+    Q8Desc g{};
+    g.A = static_cast<const uint8_t*>(a); g.lda = a4 ? lda / 2 : lda;
+    g.SA = static_cast<const uint8_t*>(a_scale); g.sa_ld = a4 ? q4_scale_cols(p.K) : q8_scale_cols(p.K);
+    g.B = static_cast<const uint8_t*>(b); g.b_seg_stride = static_cast<int64_t>(p.N) * q4_cols(p.K);
+    g.SB = static_cast<const uint8_t*>(b_scale); g.sb_ld = q4_scale_cols(p.K);
+    g.sb_seg_stride = static_cast<int64_t>(p.N) * g.sb_ld;
+    g.bias = bias;
+    g.C = c; g.ldc = c4 ? ldc / 2 : ldc;
+    g.SC = static_cast<uint8_t*>(c_scale); g.sc_ld = c4 ? q4_scale_cols(p.N) : q8_scale_cols(p.N);
+    g.out = out;
+    g.gelu = p.gelu;
+    g.fa = a4 ? kQ8E2M1 : kQ8E4M3; g.fb = kQ8E2M1;
+    g.wide = bytes || (aligned(c, 16) && ldc % piece_elems(p.out) == 0 && p.N % piece_elems(p.out) == 0);
+    g.M = p.M; g.N = p.N; g.K = p.K;
+    g.seg_offsets = offsets; g.nseg = p.groups;
+    return launch_gemm_q4(g, stream) == hipSuccess ? CLEARMOE_OK : CLEARMOE_ERR_HIP;
+}
 
 }  // namespace
 
@@ -1629,21 +1691,64 @@ int clearmoe_quantize(int dtype, int format, int block_rows, int64_t batch, int6
                       int32_t cols, const void* x, int64_t ldx, void* values, void* scales,
                       hipStream_t stream) {
     if (dtype != CLEARMOE_F32 && dtype != CLEARMOE_BF16) return CLEARMOE_ERR_UNSUPPORTED;
-    if (!byte_format(format)) return CLEARMOE_ERR_UNSUPPORTED;
-    if (block_rows != 1 && block_rows != kQ8Block) return CLEARMOE_ERR_INVALID_ARG;
+    if (!byte_format(format) && format != CLEARMOE_E2M1) return CLEARMOE_ERR_UNSUPPORTED;
+    if (block_rows != 1 && (block_rows != kQ8Block || format == CLEARMOE_E2M1)) return CLEARMOE_ERR_INVALID_ARG;
     if (cols < 1 || cols > kMaxDim || batch < 0 || rows < 0 || ldx < cols) return CLEARMOE_ERR_INVALID_ARG;
     if (batch == 0 || rows == 0) return CLEARMOE_OK;
-    // (checked so that no product overflows)
-    constexpr int64_t kMostBlocks = int64_t{1} << 31;
-    if (rows >= kMostBlocks || batch >= kMostBlocks || ldx > (int64_t{1} << 40)) return CLEARMOE_ERR_INVALID_ARG;
-    const int64_t per = block_rows == 1 ? rows : (rows + kQ8Block - 1) / kQ8Block;
-    if (batch > kMostBlocks / per || batch * per > kMostBlocks / q8_blocks(cols)) return CLEARMOE_ERR_INVALID_ARG;
+    if (!few_blocks(batch, rows, cols, ldx, format, block_rows)) return CLEARMOE_ERR_INVALID_ARG;
     if (!x || !values || !scales) return CLEARMOE_ERR_INVALID_ARG;
     if (!aligned(x, elem_size(dtype)) || !aligned(values, 16) || !aligned(scales, 4)) return CLEARMOE_ERR_INVALID_ARG;
-    if (launch_quantize(dtype, format - CLEARMOE_E4M3, block_rows, batch, rows, cols, x, ldx,
+    if (launch_quantize(dtype, q8_format(format), block_rows, batch, rows, cols, x, ldx,
                         static_cast<uint8_t*>(values), static_cast<uint8_t*>(scales), stream) != hipSuccess)
         return CLEARMOE_ERR_HIP;
     return CLEARMOE_OK;
+}
+
+int clearmoe_dequantize(int format, int block_rows, int64_t batch, int64_t rows, int32_t cols,
+                        const void* values, const void* scales, int dtype, void* y, int64_t ldy,
+                        hipStream_t stream) {
+    if (!float_type(dtype)) return CLEARMOE_ERR_UNSUPPORTED;
+    if (!byte_format(format) && format != CLEARMOE_E2M1) return CLEARMOE_ERR_UNSUPPORTED;
+    if (block_rows != 1 && (block_rows != kQ8Block || format == CLEARMOE_E2M1)) return CLEARMOE_ERR_INVALID_ARG;
+    if (cols < 1 || cols > kMaxDim || batch < 0 || rows < 0 || ldy < cols) return CLEARMOE_ERR_INVALID_ARG;
+    if (batch == 0 || rows == 0) return CLEARMOE_OK;
+    if (!few_blocks(batch, rows, cols, ldy, format, block_rows)) return CLEARMOE_ERR_INVALID_ARG;
+    if (!y || !values || !scales) return CLEARMOE_ERR_INVALID_ARG;
+    if (!aligned(y, elem_size(dtype)) || !aligned(values, 16) || !aligned(scales, 4)) return CLEARMOE_ERR_INVALID_ARG;
+    if (launch_dequantize(dtype, q8_format(format), block_rows, batch, rows, cols, static_cast<const uint8_t*>(values),
+                          static_cast<const uint8_t*>(scales), y, ldy, stream) != hipSuccess)
+        return CLEARMOE_ERR_HIP;
+    return CLEARMOE_OK;
+}
+
+int clearmoe_rms_norm(const clearmoe_norm* norm, const void* x, const void* residual, const float* weight, void* y,
+                      void* y_scale, void* sum, hipStream_t stream) {
+    if (norm == nullptr) return CLEARMOE_ERR_INVALID_ARG;
+    const clearmoe_norm& p = *norm;
+    const bool bytes = byte_format(p.out);
+    if (!float_type(p.dtype) || (!bytes && p.out != p.dtype)) return CLEARMOE_ERR_UNSUPPORTED;
+    if (p.rows < 0 || p.rows >= (int64_t{1} << 31) || p.cols < 1 || p.cols > kMaxDim) return CLEARMOE_ERR_INVALID_ARG;
+    // (a normal float32: a row of zeros then has a finite scale)
+    if (!(p.eps >= 1.17549435e-38f && p.eps <= 3.4e38f)) return CLEARMOE_ERR_INVALID_ARG;
+    const int64_t cols = bytes ? q8_cols(p.cols) : p.cols;
+    const int64_t ldx = p.ldx != 0 ? p.ldx : p.cols, ldr = p.ldr != 0 ? p.ldr : p.cols;
+    const int64_t lds = p.lds != 0 ? p.lds : p.cols, ldy = p.ldy != 0 ? p.ldy : cols;
+    constexpr int64_t most = int64_t{1} << 31;
+    if (ldx < p.cols || ldr < p.cols || lds < p.cols || ldy < cols || ldx > most || ldr > most || lds > most ||
+        ldy > most || (bytes && ldy % 16 != 0))
+        return CLEARMOE_ERR_INVALID_ARG;
+    const size_t es = elem_size(p.dtype);
+    if (p.rows > 0 && (!x || !y || (bytes && !y_scale))) return CLEARMOE_ERR_INVALID_ARG;
+    if (!aligned(x, es) || !aligned(residual, es) || !aligned(sum, es) || !aligned(weight, 4) ||
+        !aligned(y, bytes ? 16 : es) || !aligned(y_scale, 4))
+        return CLEARMOE_ERR_INVALID_ARG;
+    NormArgs a{};
+    a.x = x; a.residual = residual; a.weight = weight; a.sum = sum;
+    a.y = y; a.scale = static_cast<uint8_t*>(y_scale);
+    a.ldx = ldx; a.ldr = ldr; a.lds = lds; a.ldy = ldy;
+    a.rows = p.rows; a.cols = p.cols; a.eps = p.eps;
+    a.inv_cols = 1.0 / p.cols;
+    return launch_rms_norm(p.dtype, q8_out(p.out), a, stream) == hipSuccess ? CLEARMOE_OK : CLEARMOE_ERR_HIP;
 }
 
 int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, const void* a_scale,
@@ -1651,6 +1756,8 @@ int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, cons
                             const int32_t* offsets, void* c, void* c_scale, hipStream_t stream) {
     if (product == nullptr) return CLEARMOE_ERR_INVALID_ARG;
     const clearmoe_product& p = *product;
+    if (p.b_format == CLEARMOE_E2M1)
+        return quantized_gemm4(p, a, a_scale, b, b_scale, bias, offsets, c, c_scale, stream);
     const bool bytes = byte_format(p.out);
     if (!byte_format(p.a_format) || !byte_format(p.b_format)) return CLEARMOE_ERR_UNSUPPORTED;
     if (!bytes && p.out != CLEARMOE_F32 && p.out != CLEARMOE_BF16) return CLEARMOE_ERR_UNSUPPORTED;
@@ -1659,8 +1766,7 @@ int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, cons
         return CLEARMOE_ERR_INVALID_ARG;
     if (p.groups < 0 || p.groups > 64 || (p.gelu != 0 && p.gelu != 1) || p.reserved != 0)
         return CLEARMOE_ERR_INVALID_ARG;
-    const int out = p.out == CLEARMOE_F32 ? kQ8OutF32 : p.out == CLEARMOE_BF16 ? kQ8OutBf16
-                    : p.out == CLEARMOE_E4M3 ? kQ8OutE4M3 : kQ8OutE5M2;
+    const int out = q8_out(p.out);
     if (!q8_launch_fits(p.M, p.N, p.groups, out)) return CLEARMOE_ERR_INVALID_ARG;
     const int64_t cols = bytes ? q8_cols(p.N) : p.N;
     const int64_t lda = p.lda != 0 ? p.lda : p.K, ldc = p.ldc != 0 ? p.ldc : cols;
@@ -1683,7 +1789,7 @@ int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, cons
     g.SC = static_cast<uint8_t*>(c_scale); g.sc_ld = q8_scale_cols(p.N);
     g.out = out;
     g.gelu = p.gelu;
-    g.fa = p.a_format - CLEARMOE_E4M3; g.fb = p.b_format - CLEARMOE_E4M3;
+    g.fa = q8_format(p.a_format); g.fb = q8_format(p.b_format);
     g.wide = aligned(c, 16) && ldc % piece_elems(p.out) == 0 && p.N % piece_elems(p.out) == 0;
     g.M = p.M; g.N = p.N; g.K = p.K;
     g.seg_offsets = offsets; g.nseg = p.groups;
@@ -1691,52 +1797,71 @@ int clearmoe_quantized_gemm(const clearmoe_product* product, const void* a, cons
 }
 
 size_t clearmoe_quantized_workspace_bytes(const clearmoe_shape* shape) {
-    return check_shape(shape, true, true) == CLEARMOE_OK ? quantized_layout(*shape).total : 0;
+    return check_shape(shape, true, true) == CLEARMOE_OK ? quantized_bytes(*shape) : 0;
 }
 
 int clearmoe_quantized_ffn_forward(const clearmoe_shape* shape, const void* x, const void* W1,
                                    const void* W1_scale, const float* b1, const void* W2,
                                    const void* W2_scale, const float* b2, const int32_t* offsets,
                                    void* y, void* ws, size_t ws_bytes, hipStream_t stream) {
+    return clearmoe_quantized_ffn_forward_ex(shape, CLEARMOE_E4M3, CLEARMOE_E4M3, x, W1, W1_scale, b1, W2, W2_scale,
+                                             b2, offsets, y, ws, ws_bytes, stream);
+}
+
+int clearmoe_quantized_ffn_forward_ex(const clearmoe_shape* shape, int activations, int weights, const void* x,
+                                      const void* W1, const void* W1_scale, const float* b1, const void* W2,
+                                      const void* W2_scale, const float* b2, const int32_t* offsets,
+                                      void* y, void* ws, size_t ws_bytes, hipStream_t stream) {
     int rc = check_shape(shape, true, true);
     if (rc != CLEARMOE_OK) return rc;
     const clearmoe_shape& s = *shape;
     const size_t es = elem_size(s.dtype);
+    const bool a4 = activations == CLEARMOE_E2M1, w4 = weights == CLEARMOE_E2M1;
+    if ((!w4 && weights != CLEARMOE_E4M3) || (activations != CLEARMOE_E4M3 && !(a4 && w4)))
+        return CLEARMOE_ERR_UNSUPPORTED;
     if (!W1 || !W1_scale || !W2 || !W2_scale || (s.T > 0 && (!x || !y))) return CLEARMOE_ERR_INVALID_ARG;
     if (!aligned(W1, 16) || !aligned(W2, 16) || !aligned(x, es) || !aligned(y, es)) return CLEARMOE_ERR_INVALID_ARG;
     const void* v4[] = {W1_scale, W2_scale, b1, b2, offsets};
     for (const void* p : v4)
         if (p && !aligned(p, 4)) return CLEARMOE_ERR_INVALID_ARG;
-    const QuantizedLayout L = quantized_layout(s);
-    if (!ws || !aligned(ws, kAlign) || ws_bytes < L.total) return CLEARMOE_ERR_WORKSPACE;
+    const QuantizedLayout L = quantized_layout(s, a4);
+    if (!ws || !aligned(ws, kAlign) || ws_bytes < quantized_bytes(s)) return CLEARMOE_ERR_WORKSPACE;
     if (s.T == 0) return CLEARMOE_OK;
-    if (quantized_few(s)) {
+    // columns of a row of x or z, as a product counts them
+    auto width = [&](int n) { return static_cast<int32_t>(a4 ? q4_blocks(n) * kQ4Block : q8_cols(n)); };
+    if (w4 ? q4_few_supported(s.T, width(s.D)) && q4_few_supported(s.T, width(s.H)) : quantized_few(s)) {
         Q8Desc g{};
         g.M = s.T;
+        g.fa = a4 ? kQ8E2M1 : kQ8E4M3;
         g.seg_offsets = offsets; g.nseg = offsets ? s.E : 0;
         auto product = [&](const void* W, const void* scale, const float* bias, int N, int K, void* c) {
-            g.N = N; g.K = static_cast<int>(q8_cols(K));
-            g.B = static_cast<const uint8_t*>(W); g.b_seg_stride = static_cast<int64_t>(N) * g.K;
-            g.SB = static_cast<const uint8_t*>(scale); g.sb_ld = q8_scale_cols(K);
-            g.sb_seg_stride = q8_blocks(N) * g.sb_ld;
+            g.N = N; g.K = width(K);
+            g.B = static_cast<const uint8_t*>(W);
+            g.b_seg_stride = static_cast<int64_t>(N) * (w4 ? q4_cols(K) : g.K);
+            g.SB = static_cast<const uint8_t*>(scale); g.sb_ld = w4 ? q4_scale_cols(K) : q8_scale_cols(K);
+            g.sb_seg_stride = (w4 ? N : q8_blocks(N)) * g.sb_ld;
             g.bias = bias;
             g.C = c; g.ldc = N;
         };
+        auto launch = [&](const void* a, bool f32, int K0) {
+            return w4 ? launch_q4_few(g, a, f32, K0, stream) : launch_q8_few(g, a, f32, K0, stream);
+        };
         product(W1, W1_scale, b1, s.H, s.D, at<void>(ws, L.z));
         g.gelu = 1; g.out = kQ8OutF32;
-        CLEARMOE_STAGE(CLEARMOE_STAGE_FC1, stream, launch_q8_few(g, x, s.dtype == CLEARMOE_F32, s.D, stream));
+        CLEARMOE_STAGE(CLEARMOE_STAGE_FC1, stream, launch(x, s.dtype == CLEARMOE_F32, s.D));
         product(W2, W2_scale, b2, s.D, s.H, y);
         g.gelu = 0; g.out = s.dtype == CLEARMOE_F32 ? kQ8OutF32 : kQ8OutBf16;
-        CLEARMOE_STAGE(CLEARMOE_STAGE_DENSE_FC2, stream, launch_q8_few(g, at<void>(ws, L.z), true, s.H, stream));
+        CLEARMOE_STAGE(CLEARMOE_STAGE_DENSE_FC2, stream, launch(at<void>(ws, L.z), true, s.H));
         return CLEARMOE_OK;
     }
-    rc = clearmoe_quantize(s.dtype, CLEARMOE_E4M3, 1, 1, s.T, s.D, x, s.D, at<void>(ws, L.xv), at<void>(ws, L.xs),
+    rc = clearmoe_quantize(s.dtype, activations, 1, 1, s.T, s.D, x, s.D, at<void>(ws, L.xv), at<void>(ws, L.xs),
                            stream);
     if (rc != CLEARMOE_OK) return rc;
     clearmoe_product p{};
-    p.M = s.T; p.N = s.H; p.K = static_cast<int32_t>(q8_cols(s.D));
+    p.M = s.T; p.N = s.H; p.K = width(s.D);
     p.groups = offsets ? s.E : 0;
-    p.a_format = p.b_format = p.out = CLEARMOE_E4M3;
+    p.a_format = p.out = activations;
+    p.b_format = weights;
     p.gelu = 1;
     {
         StageScope scope(CLEARMOE_STAGE_FC1, stream);
@@ -1744,7 +1869,7 @@ int clearmoe_quantized_ffn_forward(const clearmoe_shape* shape, const void* x, c
                                      at<void>(ws, L.zv), at<void>(ws, L.zs), stream);
     }
     if (rc != CLEARMOE_OK) return rc;
-    p.N = s.D; p.K = static_cast<int32_t>(q8_cols(s.H));
+    p.N = s.D; p.K = width(s.H);
     p.out = s.dtype;
     p.gelu = 0;
     StageScope scope(CLEARMOE_STAGE_DENSE_FC2, stream);

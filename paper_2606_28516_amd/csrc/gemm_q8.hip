@@ -12,14 +12,11 @@
 // float32 promises.  Products with a float32 result therefore widen both
 // operands to bfloat16 (exactly) and run on its instructions at half the rate,
 // whose sums keep 24 bits, and apply the scales to each block's sum.
-#include "gemm_tile.h"
-#include "q8.h"
+#include "q8_tile.h"
 
 namespace clearmoe {
 
 namespace {
-
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // ---------------------------------------------------------------------------
 // A few rows: 16 rows x 16 columns, operands straight from memory into
@@ -235,8 +232,6 @@ hipError_t q8_few(const Q8Desc& g, const void* A, int K0, hipStream_t st) {
 // ---------------------------------------------------------------------------
 // Many rows: tiles through LDS.
 // ---------------------------------------------------------------------------
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
 // 32 bytes of a stage row in LDS: a stage is 128 bytes (one scale block) of k,
 // so a stage row is a whole line and its scale one byte.
 __device__ __forceinline__ i32x8 q8_lds_frag(const unsigned char* p, uint32_t off) {
@@ -248,233 +243,6 @@ __device__ __forceinline__ i32x8 q8_lds_frag(const unsigned char* p, uint32_t of
         f[i + 4] = static_cast<int>(b[i]);
     }
     return f;
-}
-
-// GELU for results that are rounded to 8 bits or bfloat16: v Phi(v) =
-// max(v, 0) - |v| Phi(-|v|) with Phi(-a) = 2^P(a), P the polynomial of degree
-// 7 that is nearest to log2 Phi(-a) on [0, 6] (4.7e-6, so GELU is off by at
-// most 3.3e-6 of itself there; further out P falls on without end): 13
-// full-rate operations' time instead of gelu_erf's 20.  fc1 + GELU over many
-// rows is bound by this vector work (50432 x 3072 x 768: 199 us with gelu_erf,
-// 141 without any).  An infinite v gives NaN, as gelu_erf does.
-__device__ __forceinline__ float q8_gelu(float v) {
-    const float a = fabsf(v);
-    float p = __builtin_fmaf(a, -1.83535093e-06f, 6.16087855e-05f);
-    p = __builtin_fmaf(a, p, -9.3060248e-04f);
-    p = __builtin_fmaf(a, p, 8.50815862e-03f);
-    p = __builtin_fmaf(a, p, -5.39604758e-02f);
-    p = __builtin_fmaf(a, p, -4.58464246e-01f);
-    p = __builtin_fmaf(a, p, -1.15125091f);
-    p = __builtin_fmaf(a, p, -9.99995318e-01f);
-    float m;                                     // (fmaxf takes two instructions: it quiets NaN first)
-    asm("v_max_f32 %0, 0, %1" : "=v"(m) : "v"(v));
-    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), m);
-}
-
-// Four floats over a scale -> four bytes (as q8_pack4, the division inside).
-template <int FMT>
-__device__ __forceinline__ uint32_t q8_pack4_over(float a, float b, float c, float d, float scale) {
-    typedef short s16x2 __attribute__((ext_vector_type(2)));
-    s16x2 v = {0, 0};
-    if constexpr (FMT == kQ8E4M3) {
-        v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, a, b, scale, false);
-        v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, c, d, scale, true);
-    } else {
-        v = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(v, a, b, scale, false);
-        v = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(v, c, d, scale, true);
-    }
-    return __builtin_bit_cast(uint32_t, v);
-}
-
-// Sums start at the bias, which saves an addition a value at the end.  Its
-// values for a wave's 32 TN columns from c are put in the lanes' order through
-// 128 TN bytes of the wave's own LDS (wb): here in registers on the way, or
-// fetched by q8_bias_dma and waited for by the caller.
-__device__ __forceinline__ gb_i32x4 q8_bias_desc(const Q8Desc& g, int seg) {
-    return gb_desc(g.bias + static_cast<int64_t>(seg) * g.N, static_cast<int64_t>(g.N) * 4);
-}
-template <int TN>
-__device__ __forceinline__ void q8_bias_dma(const Q8Desc& g, int seg, int c, int lane, uint32_t wb) {
-    const gb_i32x4 d = q8_bias_desc(g, seg);
-    static_assert(TN <= 2, "a word a lane");
-    gb_dma4(d, lane < 32 * TN ? static_cast<uint32_t>(c + lane) * 4u : kGbOob, 0, __builtin_amdgcn_readfirstlane(wb));
-}
-template <int TN>
-__device__ __forceinline__ void q8_bias_load(const Q8Desc& g, int seg, int c, int lane, unsigned char* wb) {
-    const __amdgpu_buffer_rsrc_t rb = raw_rsrc(g.bias + static_cast<int64_t>(seg) * g.N, static_cast<int64_t>(g.N) * 4);
-#pragma unroll
-    for (int h = 0; h < TN / 2; ++h)
-        reinterpret_cast<float*>(wb)[h * 64 + lane] =
-            __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, (c + h * 64 + lane) * 4, 0, 0));
-    __builtin_amdgcn_wave_barrier();
-}
-template <int TM, int TN>
-__device__ __forceinline__ void q8_start(int lane, const unsigned char* wb, f32x16 (&acc)[TM][TN]) {
-    const int lh = lane >> 5;
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const f32x4 b =
-                *reinterpret_cast<const f32x4*>(wb + 4 * (j * 32 + 16 * (h >> 1) + 8 * lh + 4 * (h & 1)));
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[i][j][4 * h + v] = b[v];
-        }
-    __builtin_amdgcn_wave_barrier();
-}
-
-// Epilogue of one wave: 32 TM rows from rw, 32 TN columns from nw.  Lane l
-// holds row i * 32 + l % 32 and, for each half h of a tile's 16 values, eight
-// consecutive columns (gb_col_of_slot).  Rows are rounded, put together in 32
-// rows of this wave's own LDS (wb) and stored as whole row pieces.  For an
-// 8-bit result, 128 / (32 TN) waves side by side share a block: they exchange
-// the rows' maxima through s_max [waves side by side][BM], between barriers
-// that all waves of the workgroup take.
-template <int TM, int TN, int OUT, int BM>
-__device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, int rw, int nw, int wn, int lane,
-                                            unsigned char* wb, float* s_max, f32x16 (&acc)[TM][TN]) {
-    constexpr bool F32 = OUT == kQ8OutF32, BF16 = OUT == kQ8OutBf16;
-    constexpr int FMT = OUT == kQ8OutE4M3 ? kQ8E4M3 : kQ8E5M2;
-    constexpr int RB = TN * 32 * (F32 ? 4 : BF16 ? 2 : 1), CH = RB / 16, RPI = 64 / CH, SHARE = 4 / TN;
-    static_assert(RB >= 32 && 64 % CH == 0 && 32 % RPI == 0, "whole rows per store");
-    const int lrow = lane & 31, lh = lane >> 5;
-    const int cols = static_cast<int>(q8_cols(g.N));
-    if (g.gelu)
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][j][v] = F32 ? gelu_erf(acc[i][j][v]) : q8_gelu(acc[i][j][v]);
-    float mx[TM];
-    if constexpr (!F32 && !BF16) {
-        // Bytes past N are zeros whatever the row holds (their sums are zeros
-        // times A: NaN where A is no number or infinite); 16 of them at most
-        // are stored.
-        if (cols != g.N && nw + 32 * TN > g.N)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (nw + j * 32 + 16 * (v >> 3) + 8 * lh + (v & 7) >= g.N)
-#pragma unroll
-                        for (int i = 0; i < TM; ++i) acc[i][j][v] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            // a lane and the one 32 further hold a row's columns; infinities
-            // (rare: the whole wave looks again) do not set the scale
-            float m = 0.0f;
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) m = fmaxf(m, fabsf(acc[i][j][v]));
-            if (__ballot(!(m < __builtin_inff())) != 0) {
-                m = 0.0f;
-#pragma unroll
-                for (int j = 0; j < TN; ++j)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) m = fmaxf(m, q8_mag(acc[i][j][v]));
-            }
-            mx[i] = fmaxf(m, __shfl_xor(m, 32));
-            if (SHARE > 1 && lh == 0) s_max[wn * BM + rw + i * 32 + lrow] = mx[i];
-        }
-        if constexpr (SHARE > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int w = 0; w < SHARE; ++w)
-                    mx[i] = fmaxf(mx[i], s_max[(wn / SHARE * SHARE + w) * BM + rw + i * 32 + lrow]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        if constexpr (F32) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const f32x4 w = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                    const int ch = j * 8 + 4 * (q >> 1) + 2 * lh + (q & 1);
-                    *reinterpret_cast<f32x4*>(wb + lrow * RB + ((ch ^ (lrow % CH)) << 4)) = w;
-                }
-        } else if constexpr (BF16) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u32x4 w;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        w[q] = pack2_bf16(acc[i][j][8 * h + 2 * q], acc[i][j][8 * h + 2 * q + 1]);
-                    const int ch = j * 4 + 2 * h + lh;
-                    *reinterpret_cast<u32x4*>(wb + lrow * RB + ((ch ^ (lrow % CH)) << 4)) = w;
-                }
-        } else {
-            const int e = q8_exponent(__float_as_uint(mx[i]), q8_top_exp(FMT));
-            const float k = q8_two_to(e);
-            const int rl = rw + i * 32 + lrow;
-            if (lh == 0 && rl < t.rows && nw % kQ8Block == 0 && nw < g.N) {
-                uint8_t* s = g.SC + (t.m_lo + rl) * g.sc_ld;
-                const int blk = nw / kQ8Block;
-                s[blk] = static_cast<uint8_t>(e + kQ8One);
-                if (nw + kQ8Block >= g.N)                       // the last block fills the row up
-                    for (int64_t p = blk + 1; p < g.sc_ld; ++p) s[p] = kQ8One;
-            }
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u32x2 w;
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int v = 8 * h + 4 * q;
-                        w[q] = q8_pack4_over<FMT>(acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2],
-                                                  acc[i][j][v + 3], k);
-                    }
-                    const int ch = j * 2 + h;
-                    *reinterpret_cast<u32x2*>(wb + lrow * RB + ((ch ^ (lrow % CH)) << 4) + 8 * lh) = w;
-                }
-        }
-        // one wave's LDS accesses complete in order: only the compiler has to
-        // keep them in place
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int it = 0; it < 32 / RPI; ++it) {
-            const int rr = it * RPI + lane / CH, ch = lane % CH;
-            const u32x4 w = *reinterpret_cast<const u32x4*>(wb + rr * RB + ((ch ^ (rr % CH)) << 4));
-            const int rl = rw + i * 32 + rr;
-            if (rl >= t.rows) continue;
-            if constexpr (F32) {
-                const int n = nw + ch * 4;
-                float* c = static_cast<float*>(g.C) + (t.m_lo + rl) * g.ldc + n;
-                if (g.wide) {
-                    if (n < g.N) *reinterpret_cast<u32x4*>(c) = w;
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (n + q < g.N) c[q] = __uint_as_float(w[q]);
-                }
-            } else if constexpr (BF16) {
-                const int n = nw + ch * 8;
-                bf16_bits* c = static_cast<bf16_bits*>(g.C) + (t.m_lo + rl) * g.ldc + n;
-                if (g.wide) {
-                    if (n < g.N) *reinterpret_cast<u32x4*>(c) = w;
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (n + q < g.N) c[q] = static_cast<bf16_bits>(w[q >> 1] >> (16 * (q & 1)));
-                }
-            } else {
-                const int n = nw + ch * 16;
-                if (n < cols)
-                    *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(g.C) + (t.m_lo + rl) * g.ldc + n) = w;
-            }
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
 }
 
 // 256 x 128 tile over four waves (64 x 128 each), two workgroups on a CU, so

@@ -1,10 +1,15 @@
-// 8-bit floating point with block scales: internal declarations of the
-// quantiser (quantize.hip) and the products (gemm_q8.hip).
+// 8- and 4-bit floating point with block scales: internal declarations of the
+// quantiser (quantize.hip), the norm with an 8-bit output (norm.hip) and the
+// products (gemm_q8.hip, gemm_q4.hip).
 //
-// A matrix of k columns is held as rows of round_up(k, 16) bytes (zeros past
+// 8 bits: a matrix of k columns is held as rows of round_up(k, 16) bytes (zeros past
 // k) and, for each block of 128 columns of a row (or of 128 rows), one byte b
 // that stands for the scale 2^(b - 127); rows of scales have
 // q8_scale_cols(k) bytes, whole 4-byte words.
+//
+// 4 bits (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives): blocks of 32
+// columns of a row, 16 bytes with the even column of a byte in its low half;
+// rows of q4_cols(k) bytes (zeros past k) and of q4_scale_cols(k) scales.
 #pragma once
 
 #include "kernels.h"
@@ -18,9 +23,14 @@ __host__ __device__ inline int64_t q8_cols(int64_t k) { return (k + 15) / 16 * 1
 __host__ __device__ inline int64_t q8_blocks(int64_t k) { return (k + kQ8Block - 1) / kQ8Block; }
 __host__ __device__ inline int64_t q8_scale_cols(int64_t k) { return (q8_blocks(k) + 3) / 4 * 4; }
 
+constexpr int kQ4Block = 32;
+__host__ __device__ inline int64_t q4_blocks(int64_t k) { return (k + kQ4Block - 1) / kQ4Block; }
+__host__ __device__ inline int64_t q4_cols(int64_t k) { return q4_blocks(k) * (kQ4Block / 2); }
+__host__ __device__ inline int64_t q4_scale_cols(int64_t k) { return (q4_blocks(k) + 3) / 4 * 4; }
+
 // Formats, as the matrix instructions number them, and output types.
-enum { kQ8E4M3 = 0, kQ8E5M2 = 1 };
-enum { kQ8OutF32 = 0, kQ8OutBf16 = 1, kQ8OutE4M3 = 2, kQ8OutE5M2 = 3 };
+enum { kQ8E4M3 = 0, kQ8E5M2 = 1, kQ8E2M1 = 4 };
+enum { kQ8OutF32 = 0, kQ8OutBf16 = 1, kQ8OutE4M3 = 2, kQ8OutE5M2 = 3, kQ8OutE2M1 = 4 };
 
 // Largest finite value 1.75 * 2^kTopExp of a format.
 __host__ __device__ constexpr int q8_top_exp(int fmt) { return fmt == kQ8E4M3 ? 8 : 15; }
@@ -35,6 +45,18 @@ __device__ __forceinline__ int q8_exponent(uint32_t u, int top) {
     return e < -126 ? -126 : e;
 }
 __device__ __forceinline__ float q8_two_to(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+// The same for e2m1 (amax <= 1.5 2^(2 + e)) of a block's largest magnitude
+// bits u, those of NaN and infinity too: 128, the scale that is no number,
+// since e2m1 has neither.
+constexpr int kQ4NaN = 128;
+__device__ __forceinline__ int q4_exponent(uint32_t u) {
+    if (u == 0) return 0;
+    if (u >= 0x7f800000u) return kQ4NaN;
+    const int e = static_cast<int>((u + 0x3fffffu) >> 23) - 127 - 2;
+    return e < -126 ? -126 : e;
+}
+// Bits of |v|, ordered as the magnitudes are, NaN above infinity.
+__device__ __forceinline__ uint32_t q4_mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 // |v| for the block's maximum: infinities and NaN do not set a scale.
 __device__ __forceinline__ float q8_mag(float v) {
     const float m = fabsf(v);
@@ -76,6 +98,22 @@ __device__ __forceinline__ void q8_load8(const T* row, int64_t c, int64_t n, flo
         }
     }
 }
+// Columns [c, c + 8) of a row, those before n.
+template <typename T>
+__device__ __forceinline__ void q8_store8(T* row, int64_t c, int64_t n, const float (&v)[8]) {
+    if (c + 8 > n) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < n) row[c + i] = Elem<T>::from_f32(v[i]);
+    } else if constexpr (sizeof(T) == 4) {
+        __builtin_memcpy(row + c, v, 32);
+    } else {
+        u32x4 a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = pack2_bf16(v[2 * i], v[2 * i + 1]);
+        __builtin_memcpy(row + c, &a, 16);
+    }
+}
 __device__ __forceinline__ float q8_mag8(const float (&v)[8]) {
     float m = 0.0f;
 #pragma unroll
@@ -88,10 +126,43 @@ __device__ __forceinline__ uint2 q8_pack8(const float (&v)[8], float s) {
                       q8_pack4<FMT>(v[4] * s, v[5] * s, v[6] * s, v[7] * s));
 }
 
+// Eight floats over 2^e (their block's; e = kQ4NaN: zeros) -> eight e2m1
+// values, the first in the lowest bits, round to nearest even.
+__device__ __forceinline__ uint32_t q4_pack8(const float (&v)[8], int e) {
+    if (e == kQ4NaN) return 0;
+    const float s = q8_two_to(-e);               // (a normal number: the product is exact)
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * s, v[1] * s, 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * s, v[3] * s, 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * s, v[5] * s, 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * s, v[7] * s, 1.0f, 3);
+}
+
 // x [batch, rows, cols] (dtype, row stride ldx elements, batches rows * ldx
-// apart) -> v, scale; block_rows 1 or 128.
+// apart) -> v, scale; block_rows 1 or 128 (e2m1: 1).
 hipError_t launch_quantize(int dtype, int fmt, int block_rows, int64_t batch, int64_t rows, int64_t cols,
                            const void* x, int64_t ldx, uint8_t* v, uint8_t* scale, hipStream_t st);
+
+// v, scale of a format -> y [batch, rows, cols] (dtype, row stride ldy).
+hipError_t launch_dequantize(int dtype, int fmt, int block_rows, int64_t batch, int64_t rows, int64_t cols,
+                             const uint8_t* v, const uint8_t* scale, void* y, int64_t ldy, hipStream_t st);
+
+// h = x (+ residual), y = h rsqrt(mean h^2 + eps) weight (norm.hip): rows of
+// dtype, y of dtype or (out: a byte format) 8-bit with scales of 1 x 128.
+struct NormArgs {
+    const void* x;
+    const void* residual;        // or null
+    const float* weight;         // [cols], or null: ones
+    void* sum;                   // h, or null
+    void* y;                     // 8 bits: rows of ldy bytes
+    uint8_t* scale;              // 8 bits: rows of q8_scale_cols(cols) bytes
+    int64_t ldx, ldr, lds, ldy;
+    int64_t rows;
+    int cols;
+    float eps;
+    double inv_cols;             // 1 / cols
+};
+hipError_t launch_rms_norm(int dtype, int out, const NormArgs& a, hipStream_t st);
 
 // C[m, n] = epi( sum over blocks of 2^(sa + sb) sum_k A[m, k] B_seg(m)[n, k] ).
 struct Q8Desc {
@@ -133,5 +204,13 @@ bool q8_launch_fits(int64_t M, int N, int groups, int out);
 constexpr int64_t kQ8FewRows = 16;       // at most: then a pass of its own costs less
 bool q8_few_supported(int64_t M, int64_t K);
 hipError_t launch_q8_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStream_t st);
+
+// The product of e4m3 or e2m1 rows (fa) and e2m1 matrices (gemm_q4.hip); every
+// stride of bytes in bytes: a row of B has q4_cols(K) of them, SB
+// q4_scale_cols(K) for each of N, a row of e2m1 results ldc.
+hipError_t launch_gemm_q4(const Q8Desc& g, hipStream_t st);
+// As launch_q8_few, the rows quantised to fa.
+bool q4_few_supported(int64_t M, int64_t K);
+hipError_t launch_q4_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStream_t st);
 
 }  // namespace clearmoe

@@ -38,6 +38,84 @@ __global__ __launch_bounds__(kThreads) void k_quantize_rows(const T* x, int64_t 
     }
 }
 
+// e2m1: 16 lanes take 128 columns, four blocks of 32, and write their bytes
+// and the word of their four scales.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_quantize4(const T* x, int64_t ldx, int64_t rows, int64_t cols,
+                                                        uint8_t* v, uint8_t* scale) {
+    const int64_t units = q8_blocks(cols), vcols = q4_cols(cols);
+    const int sub = threadIdx.x % kLanes;
+    const int64_t b = static_cast<int64_t>(blockIdx.x) * (kThreads / kLanes) + threadIdx.x / kLanes;
+    if (b >= rows * units) return;
+    const int64_t row = b / units, unit = b - row * units, c = unit * kQ8Block + sub * 8;
+    float f[8];
+    q8_load8(x + row * ldx, c, cols, f);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, q4_mag(f[i]));
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 1)));
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 2)));
+    const int e = q4_exponent(m);
+    if (c / 2 < vcols) *reinterpret_cast<uint32_t*>(v + row * vcols + c / 2) = q4_pack8(f, e);
+    // (blocks past the last have no columns: zeros, the scale 1)
+    uint32_t w = static_cast<uint32_t>(e + kQ8One) << (8 * (sub / 4));
+    w |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(w), 4));
+    w |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(w), 8));
+    if (sub == 0) reinterpret_cast<uint32_t*>(scale)[row * units + unit] = w;
+}
+
+// The value that a byte (e2m1: eight values, the word of them) stands for,
+// times 2^(s - 127).  Exact in float32, and in bfloat16 but where it falls
+// below its normal numbers.
+template <typename T, int FMT>
+__device__ __forceinline__ void q8_read8(const uint8_t* p, uint32_t s, float (&f)[8]) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    f32x2 d[4];
+    if constexpr (FMT == kQ8E2M1) {
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(p);
+        d[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, 1.0f, 0);
+        d[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, 1.0f, 1);
+        d[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, 1.0f, 2);
+        d[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, 1.0f, 3);
+    } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        const int w[2] = {static_cast<int>(u.x), static_cast<int>(u.y)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if constexpr (FMT == kQ8E4M3) {
+                d[2 * i] = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false);
+                d[2 * i + 1] = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
+            } else {
+                d[2 * i] = __builtin_amdgcn_cvt_pk_f32_bf8(w[i], false);
+                d[2 * i + 1] = __builtin_amdgcn_cvt_pk_f32_bf8(w[i], true);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        f[i] = s == 255u ? __builtin_nanf("") : __builtin_ldexpf(d[i / 2][i % 2], static_cast<int>(s) - kQ8One);
+}
+
+// Back: a thread takes eight columns.
+template <typename T, int FMT>
+__global__ __launch_bounds__(kThreads) void k_dequantize(const uint8_t* v, const uint8_t* scale, int block_rows,
+                                                         int64_t rows, int64_t first, int64_t all, int64_t cols,
+                                                         T* y, int64_t ldy) {
+    constexpr bool E2M1 = FMT == kQ8E2M1;
+    const int64_t pieces = (cols + 7) / 8;
+    const int64_t i = (first + blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= all) return;
+    const int64_t row = i / pieces, c = (i - row * pieces) * 8;         // row over all batches
+    int64_t srow = row;
+    if (block_rows != 1) {
+        const int64_t b = row / rows;
+        srow = b * ((rows + kQ8Block - 1) / kQ8Block) + (row - b * rows) / kQ8Block;
+    }
+    const uint32_t s = scale[srow * (E2M1 ? q4_scale_cols(cols) : q8_scale_cols(cols)) + c / (E2M1 ? kQ4Block : kQ8Block)];
+    float f[8];
+    q8_read8<T, FMT>(v + row * (E2M1 ? q4_cols(cols) : q8_cols(cols)) + (E2M1 ? c / 2 : c), s, f);
+    q8_store8(y + row * ldy, c, cols, f);
+}
+
 // 128 x 128 blocks: a workgroup each (from block `first` on), its values in
 // registers between the maximum and the rounding.
 template <typename T, int FMT>
@@ -108,11 +186,54 @@ hipError_t quantize(int block_rows, int64_t batch, int64_t rows, int64_t cols, c
     return hipGetLastError();
 }
 
+template <typename T>
+hipError_t quantize4(int64_t all, int64_t cols, const T* x, int64_t ldx, uint8_t* v, uint8_t* scale, hipStream_t st) {
+    constexpr int64_t PER = kThreads / kLanes;
+    const int64_t units = q8_blocks(cols), most = kMostGroups * PER / units;
+    for (int64_t r = 0; r < all; r += most) {
+        const int64_t n = all - r < most ? all - r : most, grid = (n * units + PER - 1) / PER;
+        launch_kernel(k_quantize4<T>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st, x + r * ldx, ldx, n,
+                      cols, v + r * q4_cols(cols), scale + r * q4_scale_cols(cols));
+    }
+    return hipGetLastError();
+}
+
+template <typename T, int FMT>
+hipError_t dequantize(int block_rows, int64_t batch, int64_t rows, int64_t cols, const uint8_t* v,
+                      const uint8_t* scale, T* y, int64_t ldy, hipStream_t st) {
+    const int64_t all = batch * rows * ((cols + 7) / 8), groups = (all + kThreads - 1) / kThreads;
+    for (int64_t b = 0; b < groups; b += kMostGroups) {
+        const int64_t grid = groups - b < kMostGroups ? groups - b : kMostGroups;
+        launch_kernel(k_dequantize<T, FMT>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st, v, scale,
+                      block_rows, rows, b, all, cols, y, ldy);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t dequantize(int fmt, int block_rows, int64_t batch, int64_t rows, int64_t cols, const uint8_t* v,
+                      const uint8_t* scale, void* y, int64_t ldy, hipStream_t st) {
+    T* p = static_cast<T*>(y);
+    return fmt == kQ8E4M3   ? dequantize<T, kQ8E4M3>(block_rows, batch, rows, cols, v, scale, p, ldy, st)
+           : fmt == kQ8E5M2 ? dequantize<T, kQ8E5M2>(block_rows, batch, rows, cols, v, scale, p, ldy, st)
+                            : dequantize<T, kQ8E2M1>(block_rows, batch, rows, cols, v, scale, p, ldy, st);
+}
+
 }  // namespace
+
+hipError_t launch_dequantize(int dtype, int fmt, int block_rows, int64_t batch, int64_t rows, int64_t cols,
+                             const uint8_t* v, const uint8_t* scale, void* y, int64_t ldy, hipStream_t st) {
+    if (batch == 0 || rows == 0) return hipSuccess;
+    return dtype == 0 ? dequantize<float>(fmt, block_rows, batch, rows, cols, v, scale, y, ldy, st)
+                      : dequantize<bf16_bits>(fmt, block_rows, batch, rows, cols, v, scale, y, ldy, st);
+}
 
 hipError_t launch_quantize(int dtype, int fmt, int block_rows, int64_t batch, int64_t rows, int64_t cols,
                            const void* x, int64_t ldx, uint8_t* v, uint8_t* scale, hipStream_t st) {
     if (batch == 0 || rows == 0) return hipSuccess;
+    if (fmt == kQ8E2M1)
+        return dtype == 0 ? quantize4(batch * rows, cols, static_cast<const float*>(x), ldx, v, scale, st)
+                          : quantize4(batch * rows, cols, static_cast<const bf16_bits*>(x), ldx, v, scale, st);
     if (dtype == 0) {
         const float* p = static_cast<const float*>(x);
         return fmt == kQ8E4M3 ? quantize<float, kQ8E4M3>(block_rows, batch, rows, cols, p, ldx, v, scale, st)

@@ -1600,7 +1600,7 @@ int quantized_gemm4(const clearmoe_product& p, const void* a, const void* a_scal
     if (p.groups < 0 || p.groups > 64 || (p.gelu != 0 && p.gelu != 1) || p.reserved != 0)
         return CLEARMOE_ERR_INVALID_ARG;
     const int out = q8_out(p.out);
-    if (!q8_launch_fits(p.M, p.N, p.groups, out)) return CLEARMOE_ERR_INVALID_ARG;
+    if (!q4_launch_fits(p.M, p.N, p.groups)) return CLEARMOE_ERR_INVALID_ARG;
     const int64_t cols = c4 ? q4_blocks(p.N) * kQ4Block : bytes ? q8_cols(p.N) : p.N;
     const int64_t lda = p.lda != 0 ? p.lda : p.K, ldc = p.ldc != 0 ? p.ldc : cols;
     if (lda < p.K || lda > kMaxStride || lda % unit != 0) return CLEARMOE_ERR_INVALID_ARG;

@@ -12,6 +12,8 @@
 // with a float32 result take two instructions, one for the rows' values from 2
 // on (products from 2^-3 to 2688, in whole eighths) and one for those below
 // (up to 11.25, in whole 2^-10), each of which cuts nothing.
+#include <type_traits>
+
 #include "q8_tile.h"
 
 namespace clearmoe {
@@ -54,6 +56,11 @@ __device__ __forceinline__ uint32_t q4_scale_mask(int blocks) {
     return blocks >= 4 ? 0xffffffffu : blocks <= 0 ? 0u : (1u << (8 * blocks)) - 1;
 }
 __device__ __forceinline__ uint32_t q4_masked(uint32_t w, uint32_t mask) { return (w & mask) | (0x7f7f7f7fu & ~mask); }
+
+template <int N>
+__device__ __forceinline__ void q4_words(const unsigned char* p, uint32_t (&w)[N]) {
+    __builtin_memcpy(w, __builtin_assume_aligned(p, N * 4), N * 4);
+}
 
 // How the instructions lay out k (measured): of a 4-bit operand, lane group g
 // holds values 32 g .. 32 g + 31, of an 8-bit one 16 g .. 16 g + 15 and the
@@ -309,8 +316,11 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
     constexpr int SSIZE = 2 * SCALES > WN * BM * 4 ? 2 * SCALES : WN * BM * 4;
     constexpr int GROUP = SOFF + SSIZE, SUMS = NW * 64 * TM * TN * 64;
     static_assert(SOFF >= EPI && (KG == 1 || SOFF >= SUMS), "the epilogue's rows and the sums fit the stages");
-    constexpr int BIAS = TN <= 2 ? 256 : TN * 128;                      // whole loads of a word a lane
-    __shared__ __attribute__((aligned(1024))) unsigned char smem_all[KG * GROUP + NW * BIAS];
+    // the bias waits in the second piece's place, which is filled after the
+    // first stage: whole loads of a word a lane
+    constexpr int BIAS = TN <= 2 ? 256 : TN * 128, BOFF = SOFF + SCALES;
+    static_assert(NW * BIAS <= SCALES, "a wave's columns each");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem_all[KG * GROUP];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wave_all / NW, wave = wave_all % NW;
@@ -394,7 +404,7 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
                          __builtin_amdgcn_readfirstlane(at + SCA + i * 1024));
     };
     // the bias of the wave's columns (zeros past N)
-    const uint32_t boff = KG * GROUP + wave * BIAS;
+    const uint32_t boff = BOFF + wave * BIAS;
     if (g.bias != nullptr && kg == 0) {
         const gb_i32x4 d = q8_bias_desc(g, t.seg);
 #pragma unroll
@@ -416,9 +426,10 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
         ob[s] = static_cast<uint32_t>(STAGE_A + (wn * TN * 32 + bcol) * SB + (((2 * s + lh) ^ gb_swz<SB>(bcol)) << 4));
     }
     u32x4 fa[2][A4 ? 1 : 2][TM], fb[2][TN];
-    // scale words by the stage's parity, a lane's own byte first
+    // scale words of the stage at hand, a lane's own byte first, and of the
+    // next as they are read
     constexpr int SW = KS / 128, SWA = A4 ? SW : 1;
-    uint32_t sa[2][SWA][TM], sb[2][SW][TN];
+    uint32_t sa[TM][SWA], sb[TN][SW], ra[TM][SWA], rb[TN][SW];
     auto read = [&](int b, int s) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
@@ -430,37 +441,46 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
                 fa[s & 1][1][i] = *reinterpret_cast<const u32x4*>(smem + b * STAGE + (oa[s] ^ 32u) + i * 32 * SA);
         }
     };
-    auto read_scales = [&](int s, int b) {
-        const int kt = stage_of(s), at = s % PER;                       // stage of its piece
+    auto read_scales = [&](int s) {
         const unsigned char* p = smem + SOFF + ((s / PER) & 1) * SCALES;
+        const int at = s % PER;                                         // stage of its piece
 #pragma unroll
-        for (int w = 0; w < SW; ++w) {
-            const uint32_t mask = q4_scale_mask(blocks - (kt * SW + w) * 4);
+        for (int j = 0; j < TN; ++j)
+            q4_words<SW>(p + SCA + (wn * TN * 32 + j * 32 + bcol) * 16 + at * SW * 4, rb[j]);
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-                sb[b][w][j] = q4_masked(*reinterpret_cast<const uint32_t*>(
-                                            p + SCA + (wn * TN * 32 + j * 32 + bcol) * 16 + (at * SW + w) * 4),
-                                        mask) >> (8 * lh);
-            if constexpr (A4) {
+        for (int i = 0; i < TM; ++i)
+            q4_words<SWA>(p + (wm * TM * 32 + i * 32 + lrow) * (A4 ? 16 : 4) + (A4 ? at * SW * 4 : 0), ra[i]);
+    };
+    // what was read of stage s; past the last block, scales of 1
+    auto take_scales = [&](int s) {
+        const int have = blocks - stage_of(s) * SW * 4;
+        if (have < SW * 4) {
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
-                    sa[b][w][i] = q4_masked(*reinterpret_cast<const uint32_t*>(
-                                                p + (wm * TM * 32 + i * 32 + lrow) * 16 + (at * SW + w) * 4),
-                                            mask) >> (8 * lh);
+            for (int w = 0; w < SW; ++w) {
+                const uint32_t mask = q4_scale_mask(have - w * 4);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) rb[j][w] = q4_masked(rb[j][w], mask);
+                if constexpr (A4)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) ra[i][w] = q4_masked(ra[i][w], mask);
             }
         }
-        if constexpr (!A4)
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-                sa[b][0][i] = *reinterpret_cast<const uint32_t*>(p + (wm * TM * 32 + i * 32 + lrow) * 4) >> (8 * at);
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int w = 0; w < SW; ++w) sb[j][w] = rb[j][w] >> (8 * lh);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int w = 0; w < SWA; ++w) sa[i][w] = ra[i][w] >> (A4 ? 8 * lh : 8 * (s % PER));
     };
     gb_wait_barrier<0>();                        // the bias and two stages have landed
     f32x16 acc[TM][TN];
-    if (g.bias != nullptr && kg == 0) q8_start(lane, smem_all + boff, acc);
+    if (g.bias != nullptr && kg == 0) q8_start(lane, smem + boff, acc);
     else gb_zero(acc);
     read(0, 0);
-    read_scales(0, 0);
-    auto mm = [&](auto step, int b) {
+    read_scales(0);
+    auto mm = [&](auto step) {
         constexpr int S = decltype(step)::value, W = S / 2, OB = 2 * (S % 2), OA = A4 ? OB : 0;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -468,8 +488,8 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
                 const i32x8 a = A4 ? q4_wide(fa[S & 1][0][i]) : q4_join(fa[S & 1][0][i], fa[S & 1][A4 ? 0 : 1][i]);
-                acc[i][j] = q4_mfma32<FA, WIDE, OB, OA>(q4_wide(fb[S & 1][j]), a, acc[i][j], sb[b][W][j],
-                                                        sa[b][A4 ? W : 0][i]);
+                acc[i][j] = q4_mfma32<FA, WIDE, OB, OA>(q4_wide(fb[S & 1][j]), a, acc[i][j], sb[j][W],
+                                                        sa[i][A4 ? W : 0]);
             }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -479,6 +499,7 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
             const int s = s0 + b;
             if (s >= most) break;
             const bool have = stage_of(s) < nk, next = s + 1 < most;
+            take_scales(s);
             auto step = [&](auto at) {
                 constexpr int S = decltype(at)::value;
                 if constexpr (S + 1 < STEPS) {
@@ -488,10 +509,10 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
                     // done reading stage s's buffer, which takes s + 2
                     gb_wait_barrier<0>();
                     read(b ^ 1, 0);
-                    read_scales(s + 1, b ^ 1);
+                    read_scales(s + 1);
                     if (s + 2 < most) dma(s + 2, b);
                 }
-                if (have) mm(at, b);
+                if (have) mm(at);
             };
             step(std::integral_constant<int, 0>{});
             step(std::integral_constant<int, 1>{});
@@ -546,15 +567,69 @@ hipError_t q4_tile(const Q8Desc& g, hipStream_t st) {
     return hipGetLastError();
 }
 
+// Tiles of bm x bn of a product; a group ends inside a tile: half a tile more.
+int64_t q4_tiles(const Q8Desc& g, int bm, int bn) {
+    const int64_t groups = g.seg_offsets != nullptr ? g.nseg : 0;
+    return ((g.M + bm - 1) / bm + groups / 2) * ((g.N + bn - 1) / bn);
+}
+
+// Which kernel: by the number of tiles, that is by how well each fills the
+// chip's 256 CUs, and by k.  Times in us on an MI355X (calls in a row, N x K):
+//   4-bit rows, bfloat16          rows of A   64     512    2048    8192   32768
+//     1536 x 384    16 x 16 (rows)          3.7     6.7    20.4
+//                   64 x 64 (small)         3.9     4.2     9.9    34.4     130
+//                   64 x 128 (wide)         4.0     4.3     5.6    13.2    43.2
+//                   128 x 128, 128 of k     4.7     4.9     5.6     9.3    26.7
+//                   128 x 128, 256 of k     4.8     5.0     5.8    11.2    30.3
+//                   256 x 256               7.1     8.3     8.9    10.7    29.9
+//     1024 x 4096   16 x 16                 6.2    30.4     114
+//                   64 x 64                 6.6     7.1    15.0    59.4     214
+//                   64 x 128                9.7     9.9    11.6    31.6     122
+//                   128 x 128, 128 of k    15.8    16.0    16.7    28.7     109
+//                   128 x 128, 256 of k    12.9    13.2    13.9    24.1    89.6
+//                   256 x 256              26.6    28.0    28.4    31.1    77.8
+//   the same, GELU, to 4 bits
+//     4096 x 1024   128 x 128, 256 of k     7.3     7.6    10.1    34.3     132
+//                   128 x 256              11.3    11.5    12.5    32.4     123
+//                   256 x 256              14.9    15.5    15.8    32.6     129
+//   8-bit rows, bfloat16
+//     1536 x 384    64 x 128                4.1     4.3     5.7    13.9    45.0
+//                   128 x 128               5.0     5.3     6.0    11.7    33.9
+//                   128 x 256               6.9     7.1     7.8    11.5    30.0
+//     1024 x 4096   64 x 128               13.9    14.1    16.1    46.0     178
+//                   128 x 128              19.3    19.6    20.1    34.2     131
+//                   128 x 256              30.2    30.5    31.0    35.2     119
+enum Q4Kernel { kQ4Rows, kQ4Small, kQ4Wide, kQ4Middle, kQ4Deep, kQ4Large };
+template <int FA, int OUT>
+Q4Kernel q4_choose(const Q8Desc& g) {
+    constexpr bool A4 = FA == kQ8E2M1, FLOAT = OUT == kQ8OutF32 || OUT == kQ8OutBf16;
+    if (FLOAT && q4_tiles(g, 16, 16) <= 320) return kQ4Rows;
+    if (OUT != kQ8OutE4M3 && q4_tiles(g, 64, 64) <= 256) return kQ4Small;
+    if (q4_tiles(g, 64, 128) <= (A4 ? 400 : 512)) return kQ4Wide;
+    if (OUT == kQ8OutF32) return A4 && g.K > 512 ? kQ4Deep : kQ4Middle;
+    if (!A4) return q4_tiles(g, 128, 256) >= 384 ? kQ4Large : kQ4Middle;
+    if (g.K <= 512) return kQ4Middle;
+    return (FLOAT ? q4_tiles(g, 256, 256) >= 240 : q4_tiles(g, 128, 256) >= 400) ? kQ4Large : kQ4Deep;
+}
+
 template <int FA, int OUT>
 hipError_t q4_launch(const Q8Desc& g, hipStream_t st) {
-    if constexpr (OUT == kQ8OutF32 || OUT == kQ8OutBf16) {
-        if (g.M <= 16) {
-            if constexpr (OUT == kQ8OutF32) return q4_rows<FA, float>(g, st);
-            else return q4_rows<FA, bf16_bits>(g, st);
-        }
-    }
-    return q4_tile<1, 2, 2, 1, 2, FA == kQ8E2M1 ? 256 : 128, FA, OUT, 2>(g, st);
+    constexpr bool A4 = FA == kQ8E2M1, F32 = OUT == kQ8OutF32, BF16 = OUT == kQ8OutBf16;
+    constexpr int KS = A4 ? 256 : 128;
+    const Q4Kernel kernel = q4_choose<FA, OUT>(g);
+    if constexpr (F32 || BF16)
+        if (kernel == kQ4Rows) return q4_rows<FA, typename std::conditional<F32, float, bf16_bits>::type>(g, st);
+    if constexpr (OUT != kQ8OutE4M3)
+        if (kernel == kQ4Small) return q4_tile<2, 2, 2, 1, 1, KS, FA, OUT, 2>(g, st);
+    if (kernel == kQ4Wide) return q4_tile<1, 2, 2, 1, 2, KS, FA, OUT, 2>(g, st);
+    if constexpr (A4)
+        if (kernel == kQ4Deep) return q4_tile<1, 2, 2, 2, 2, 256, FA, OUT, 2>(g, st);
+    if constexpr (A4 && BF16)
+        if (kernel == kQ4Large) return q4_tile<1, 2, 4, 4, 2, 256, FA, OUT, 2>(g, st);
+    if constexpr (!F32 && !(A4 && BF16))
+        if (kernel == kQ4Large) return q4_tile<1, 2, 2, 2, 4, 128, FA, OUT, 2>(g, st);
+    // three workgroups on a CU (but for the split rows' registers)
+    return q4_tile<1, 2, 2, 2, 2, 128, FA, OUT, F32 && !A4 ? 2 : 3>(g, st);
 }
 
 template <int FA>
@@ -577,6 +652,11 @@ hipError_t q4_few_out(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStr
 
 }  // namespace
 
+bool q4_launch_fits(int64_t M, int N, int groups) {
+    // 128 x 128 tiles over 256 threads at the least (smaller ones are for few
+    // of them; the grid is rounded up to whole XCDs)
+    return ((M + 127) / 128 + groups) * q8_blocks(N) <= (int64_t{1} << 32) / 256 - kGbXcds;
+}
 bool q4_few_supported(int64_t M, int64_t K) {
     const int64_t rows = M < 16 ? M : 16;
     return M <= kQ8FewRows && rows * (q4_few_pitch(kQ8E4M3, K) + q4_few_spitch(kQ8E4M3, K)) <= kQ4FewLds;

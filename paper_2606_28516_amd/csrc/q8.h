@@ -209,6 +209,8 @@ hipError_t launch_q8_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hip
 // stride of bytes in bytes: a row of B has q4_cols(K) of them, SB
 // q4_scale_cols(K) for each of N, a row of e2m1 results ldc.
 hipError_t launch_gemm_q4(const Q8Desc& g, hipStream_t st);
+// Whether the product fits one launch.
+bool q4_launch_fits(int64_t M, int N, int groups);
 // As launch_q8_few, the rows quantised to fa.
 bool q4_few_supported(int64_t M, int64_t K);
 hipError_t launch_q4_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStream_t st);

@@ -48,6 +48,17 @@ __device__ __forceinline__ uint32_t q8_pack4_over(float a, float b, float c, flo
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// Eight floats over a scale -> eight e2m1 values (as q4_pack8, the division
+// inside).
+__device__ __forceinline__ uint32_t q4_pack8_over(float a, float b, float c, float d, float e, float f, float g,
+                                                  float h, float scale) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, b, scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, c, d, scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e, f, scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, g, h, scale, 3);
+}
+
 // Sums start at the bias, which saves an addition a value at the end.  Its
 // values for a wave's 32 TN columns from c are put in the lanes' order through
 // 128 TN bytes of the wave's own LDS (wb): here in registers on the way, or
@@ -180,28 +191,36 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
             // hold a row's.  (Columns past N are zeros, but where the row is
             // no number, and then so is its last block.)
             const int rl = rw + i * 32 + lrow;
+            uint32_t scales = 0;
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                uint32_t m = 0;
+                // the largest magnitude; NaN if one of them is
+                float m = 0.0f;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) m = max(m, q4_mag(acc[i][j][v]));
-                m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
-                const int e = q4_exponent(m), n = nw + j * 32;
+                for (int v = 0; v < 16; v += 2)
+                    m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(acc[i][j][v]), fabsf(acc[i][j][v + 1])), m);
+                m = __builtin_elementwise_maximum(m, __shfl_xor(m, 32));
+                const int e = nw + j * 32 < g.N ? q4_exponent(q4_mag(m)) : 0;
+                const float k = e == kQ4NaN ? 1.0f : q8_two_to(e);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float p[8];
-#pragma unroll
-                    for (int v = 0; v < 8; ++v) p[v] = acc[i][j][8 * h + v];
+                    const uint32_t w =
+                        q4_pack8_over(acc[i][j][8 * h], acc[i][j][8 * h + 1], acc[i][j][8 * h + 2], acc[i][j][8 * h + 3],
+                                      acc[i][j][8 * h + 4], acc[i][j][8 * h + 5], acc[i][j][8 * h + 6],
+                                      acc[i][j][8 * h + 7], k);
                     *reinterpret_cast<uint32_t*>(wb + lrow * RB + ((j ^ (lrow % CH)) << 4) + 8 * h + 4 * lh) =
-                        q4_pack8(p, e);
+                        e == kQ4NaN ? 0u : w;
                 }
-                if (lh == 0 && rl < t.rows && n < g.N) {
-                    uint8_t* s = g.SC + (t.m_lo + rl) * g.sc_ld;
-                    const int blk = n / kQ4Block;
-                    s[blk] = static_cast<uint8_t>(e + kQ8One);
-                    if (n + kQ4Block >= g.N)                    // the last block fills the row up
-                        for (int64_t p = blk + 1; p < g.sc_ld; ++p) s[p] = kQ8One;
-                }
+                scales |= static_cast<uint32_t>(e + kQ8One) << (8 * j);
+            }
+            // TN scales side by side; the last ones fill the row up
+            if (lh == 0 && rl < t.rows && nw < g.N) {
+                uint8_t* s = g.SC + (t.m_lo + rl) * g.sc_ld + nw / kQ4Block;
+                if constexpr (TN == 4) *reinterpret_cast<uint32_t*>(s) = scales;
+                else if constexpr (TN == 2) *reinterpret_cast<uint16_t*>(s) = static_cast<uint16_t>(scales);
+                else *s = static_cast<uint8_t>(scales);
+                if (TN < 4 && nw + TN * 32 >= g.N)
+                    for (int64_t p = nw / kQ4Block + TN; p < g.sc_ld; ++p) g.SC[(t.m_lo + rl) * g.sc_ld + p] = kQ8One;
             }
         } else {
             const int e = q8_exponent(__float_as_uint(mx[i]), q8_top_exp(FMT));

@@ -533,7 +533,7 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
 # 8-bit formats, and the C ABI's numbers of every output type; the 4-bit format
 # (two values a byte)
 _FORMATS = {torch.float8_e4m3fn: 2, torch.float8_e5m2: 3}
-_E2M1 = torch.float4_e2m1fn_x2
+_E2M1, _E8M0 = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu
 _OUTS = {torch.float32: F32, torch.bfloat16: BF16, **_FORMATS, _E2M1: 5}
 
 
@@ -576,17 +576,20 @@ def quantize(x, fmt=torch.float8_e4m3fn, block_rows: int = 1, stream=None):
     fmt torch.float4_e2m1fn_x2: 4 bits, blocks of 1 x 32 (block_rows 1), values
     [..., rows, 16 ceil(cols / 32)] of two each, the even column in the low
     half; a block with a NaN or infinite value has a NaN scale."""
-    if x.dim() not in (2, 3):
+    shape = x.shape
+    if len(shape) == 2:
+        (rows, cols), batch, lead = shape, 1, ()
+    elif len(shape) == 3:
+        batch, rows, cols = shape
+        lead = (batch,)
+    else:
         raise ClearMoEError("quantize takes [rows, cols] or [batch, rows, cols]")
-    lead = x.shape[:-2]
-    batch = x.shape[0] if lead else 1
-    rows, cols = x.shape[-2:]
-    ldx = _row_stride(x)
+    ldx = cols if x.is_contiguous() else _row_stride(x)
     st = _queue(x.get_device(), stream)
     dt, code = _dt(x), _format(fmt)
     nr = rows if block_rows == 1 else -(-rows // 128)
     v = _empty(x, (*lead, rows, _value_cols(cols, fmt)), fmt, stream)
-    s = _empty(x, (*lead, nr, _scale_cols(cols, fmt)), torch.float8_e8m0fnu, stream)
+    s = _empty(x, (*lead, nr, _scale_cols(cols, fmt)), _E8M0, stream)
     rc = lib().clearmoe_quantize(dt, code, block_rows, batch, rows, cols, x.data_ptr(), ldx, v.data_ptr(),
                                  s.data_ptr(), st)
     _check(rc, "clearmoe_quantize")
@@ -597,23 +600,29 @@ def dequantize(values, scale, cols: Optional[int] = None, dtype=torch.bfloat16, 
                out: Optional[torch.Tensor] = None, stream=None):
     """clearmoe_dequantize: what quantize's result stands for, [..., rows, cols]
     in float32 or bfloat16 (cols: as x had; default: the values' padded rows)."""
-    if values.dim() not in (2, 3):
+    shape = values.shape
+    if len(shape) not in (2, 3):
         raise ClearMoEError("dequantize takes [rows, .] or [batch, rows, .]")
-    fmt, lead, rows = values.dtype, values.shape[:-2], values.shape[-2]
-    code, dev = _format(fmt), values.get_device()
-    if dtype not in (torch.float32, torch.bfloat16):
+    batch, rows, lead = (1, shape[0], ()) if len(shape) == 2 else (shape[0], shape[1], (shape[0],))
+    fmt, dev = values.dtype, values.get_device()
+    code = _format(fmt)
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
         raise ClearMoEError(f"unsupported dtype {dtype}")
     if cols is None:
-        cols = values.shape[-1] * (2 if fmt is _E2M1 else 1)
+        cols = shape[-1] * (2 if fmt is _E2M1 else 1)
     nr = rows if block_rows == 1 else -(-rows // 128)
-    args = (_shaped(values, fmt, (*lead, rows, _value_cols(cols, fmt)), "values", dev),
-            _shaped(scale, torch.float8_e8m0fnu, (*lead, nr, _scale_cols(cols, fmt)), "scale", dev))
+    vp = _shaped(values, fmt, (*lead, rows, _value_cols(cols, fmt)), "values", dev)
+    sp = _shaped(scale, _E8M0, (*lead, nr, _scale_cols(cols, fmt)), "scale", dev)
     st = _queue(dev, stream)
-    y = _empty(values, (*lead, rows, cols), dtype, stream) if out is None else out
-    if y.dtype != dtype or y.shape != (*lead, rows, cols) or y.get_device() != dev:
-        raise ClearMoEError(f"out must be {dtype} {(*lead, rows, cols)} on the values' device")
-    rc = lib().clearmoe_dequantize(code, block_rows, values.shape[0] if lead else 1, rows, cols, *args, _OUTS[dtype],
-                                   y.data_ptr(), _row_stride(y, "rows of out"), st)
+    ldy = cols
+    if out is None:
+        y = _empty(values, (*lead, rows, cols), dtype, stream)
+    else:
+        y = out
+        if y.dtype is not dtype or y.shape != (*lead, rows, cols) or y.get_device() != dev:
+            raise ClearMoEError(f"out must be {dtype} {(*lead, rows, cols)} on the values' device")
+        ldy = _row_stride(y, "rows of out")
+    rc = lib().clearmoe_dequantize(code, block_rows, batch, rows, cols, vp, sp, _OUTS[dtype], y.data_ptr(), ldy, st)
     _check(rc, "clearmoe_dequantize")
     return y
 
@@ -626,36 +635,35 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, out_dtype=None,
     or an 8-bit format: then values and scales as quantize returns them.
     Returns y, or (values, scales); with a residual or sum_out also h, last (a
     new tensor, or sum_out, which may be x or residual itself)."""
-    if x.dim() != 2:
+    shape, xt = x.shape, x.dtype
+    if len(shape) != 2:
         raise ClearMoEError("rms_norm takes x [rows, cols]")
-    rows, cols = x.shape
-    dt, dev, xt = _dt(x), x.get_device(), x.dtype
-    ot = xt if out_dtype is None else out_dtype
-    byte = ot in _FORMATS
-    if not byte and ot != xt:
+    rows, cols = shape
+    dt, dev, ot = _dt(x), x.get_device(), xt if out_dtype is None else out_dtype
+    byte = ot is not xt
+    if byte and ot not in _FORMATS:
         raise ClearMoEError(f"out_dtype must be {xt} or an 8-bit format, not {ot}")
     st = _queue(dev, stream)
-    if weight is not None:
-        weight = _shaped(weight, torch.float32, (cols,), "weight", dev)
+    wp = None if weight is None else _shaped(weight, torch.float32, (cols,), "weight", dev)
+    yshape = (rows, _value_cols(cols)) if byte else shape
+    for t, what, d, size in ((residual, "residual", xt, shape), (sum_out, "sum_out", xt, shape), (out, "out", ot, yshape)):
+        if t is not None and (t.dtype is not d or t.shape != size or t.get_device() != dev):
+            raise ClearMoEError(f"{what} must be {d} {tuple(size)} on x's device, not {t.dtype} {tuple(t.shape)}")
+    plain = x if stream is None and x.is_contiguous() else None         # (empty_like costs less)
     if sum_out is None and residual is not None:
-        sum_out = _empty(x, (rows, cols), xt, stream)
-    yc = _value_cols(cols) if byte else cols
-    y = _empty(x, (rows, yc), ot, stream) if out is None else out
-    for t, what, c, d in ((residual, "residual", cols, xt), (sum_out, "sum_out", cols, xt), (y, "out", yc, ot)):
-        if t is not None and (t.dtype is not d or t.shape != (rows, c) or t.get_device() != dev):
-            raise ClearMoEError(f"{what} must be {d} {(rows, c)} on x's device, not {t.dtype} {tuple(t.shape)}")
-    ys = _empty(x, (rows, _scale_cols(cols)), torch.float8_e8m0fnu, stream) if byte else None
-    p = Norm(rows, cols, dt, _OUTS[ot], eps, _row_stride(x, "rows of x"),
-             0 if residual is None else _row_stride(residual, "rows of residual"),
-             0 if sum_out is None else _row_stride(sum_out, "rows of sum_out"), _row_stride(y, "rows of out"))
-    rc = lib().clearmoe_rms_norm(ctypes.byref(p), x.data_ptr(), None if residual is None else residual.data_ptr(),
-                                 weight, y.data_ptr(), None if ys is None else ys.data_ptr(),
+        sum_out = torch.empty_like(x) if plain is not None else _empty(x, (rows, cols), xt, stream)
+    y = out if out is not None else torch.empty_like(x) if plain is not None and not byte else _empty(x, yshape, ot, stream)
+    ys = _empty(x, (rows, _scale_cols(cols)), _E8M0, stream) if byte else None
+    ld = [0 if t is None or t.is_contiguous() else _row_stride(t, what)
+          for t, what in ((x, "rows of x"), (residual, "rows of residual"), (sum_out, "rows of sum_out"), (y, "rows of out"))]
+    p = Norm(rows, cols, dt, _OUTS[ot], eps, *ld)
+    rc = lib().clearmoe_rms_norm(ctypes.byref(p), x.data_ptr(), None if residual is None else residual.data_ptr(), wp,
+                                 y.data_ptr(), None if ys is None else ys.data_ptr(),
                                  None if sum_out is None else sum_out.data_ptr(), st)
     _check(rc, "clearmoe_rms_norm")
-    r = (y, ys) if byte else (y,)
-    if sum_out is not None:
-        r += (sum_out,)
-    return r if len(r) > 1 else y
+    if sum_out is None:
+        return (y, ys) if byte else y
+    return (y, ys, sum_out) if byte else (y, sum_out)
 
 
 def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offsets=None,
@@ -673,32 +681,37 @@ def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offset
     or in 4 bits too, of as many columns before their padding; out_dtype
     float32, bfloat16, e4m3 or 4 bits.  Sums of 4-bit a hold every product."""
     M, K = a.shape
-    E = 0 if offsets is None else b.shape[0]
-    lead = (E,) if E else ()
-    N = b.shape[-2]
-    four, a4, c4 = b.dtype is _E2M1, a.dtype is _E2M1, out_dtype is _E2M1
-    fa, fb = _format(a.dtype), _format(b.dtype)
-    if a4:
-        K *= 2
-    kb = _value_cols(K, _E2M1) if four else K
-    if b.shape != (*lead, N, kb):
-        raise ClearMoEError(f"b must be [{'E, ' if E else ''}N, {kb}], not {tuple(b.shape)}")
-    byte = out_dtype in _FORMATS or c4
-    if out_dtype not in _OUTS:
+    fa, fb = _OUTS.get(a.dtype, 0), _OUTS.get(b.dtype, 0)
+    if fa < 2 or fb < 2:
+        raise ClearMoEError(f"unsupported 8- or 4-bit format {a.dtype if fa < 2 else b.dtype}")
+    four, out_code, shape = fb == 5, _OUTS.get(out_dtype, -1), b.shape
+    if out_code < 0:
         raise ClearMoEError(f"unsupported dtype {out_dtype}")
-    cols, e8 = _value_cols(N, out_dtype) if byte else N, torch.float8_e8m0fnu
-    sbs = (*lead, N, _scale_cols(K, _E2M1)) if four else (*lead, -(-N // 128), _scale_cols(K))
-    p = Product(M, N, K, E, fa, fb, _OUTS[out_dtype], 1 if gelu else 0, 0, 0, 0)
+    if fa == 5:
+        K *= 2
+    lead = () if offsets is None else (shape[0],)
+    E, N, kb = (lead[0] if lead else 0), shape[-2], (_value_cols(K, _E2M1) if four else K)
+    if shape != (*lead, N, kb):
+        raise ClearMoEError(f"b must be [{'E, ' if lead else ''}N, {kb}], not {tuple(shape)}")
     dev = a.get_device()
-    args = (_ptr(a, dev), _shaped(a_scale, e8, (M, _scale_cols(K, a.dtype)), "a_scale", dev), _ptr(b, dev),
-            _shaped(b_scale, e8, sbs, "b_scale", dev),
-            _shaped_or_none(bias, torch.float32, (*lead, N), "bias", dev),
-            _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets", dev))
+    ap, bp = _ptr(a, dev), _ptr(b, dev)
+    sap = _shaped(a_scale, _E8M0, (M, _scale_cols(K, a.dtype)), "a_scale", dev)
+    sbp = _shaped(b_scale, _E8M0, (*lead, N, _scale_cols(K, _E2M1)) if four else (*lead, -(-N // 128), _scale_cols(K)),
+                  "b_scale", dev)
+    biasp = None if bias is None else _shaped(bias, torch.float32, (*lead, N), "bias", dev)
+    offp = None if offsets is None else _shaped(offsets, torch.int32, (E + 1,), "offsets", dev)
     st = _queue(dev, stream)
-    c = _empty(a, (M, cols), out_dtype, stream) if out is None else out
-    cs = _empty(a, (M, _scale_cols(N, out_dtype)), e8, stream) if byte else None
-    rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), *args, _shaped(c, out_dtype, (M, cols), "out", dev),
-                                       _ptr(cs, dev), st)
+    byte = out_code >= 2
+    cols = _value_cols(N, out_dtype) if byte else N
+    if out is None:
+        c = _empty(a, (M, cols), out_dtype, stream)
+        cp = c.data_ptr()
+    else:
+        c, cp = out, _shaped(out, out_dtype, (M, cols), "out", dev)
+    cs = _empty(a, (M, _scale_cols(N, out_dtype)), _E8M0, stream) if byte else None
+    p = Product(M, N, K, E, fa, fb, out_code, 1 if gelu else 0, 0, 0, 0)
+    rc = lib().clearmoe_quantized_gemm(ctypes.byref(p), ap, sap, bp, sbp, biasp, offp, cp,
+                                       None if cs is None else cs.data_ptr(), st)
     _check(rc, "clearmoe_quantized_gemm")
     return (c, cs) if byte else c
 
@@ -721,27 +734,32 @@ def quantized_ffn_forward(x, W1, W1_scale, b1, W2, W2_scale, b2, offsets=None,
     groups are left as out had them).  activations: what x and the hidden
     values are rounded to, e4m3 or, with 4-bit weights, 4 bits too."""
     T, D = x.shape
-    lead = () if offsets is None else (W1.shape[0],)
-    E, H = (lead[0] if lead else 1), W1.shape[-2]
-    fmt = _E2M1 if W1.dtype is _E2M1 else torch.float8_e4m3fn
-    e8, f32 = torch.float8_e8m0fnu, torch.float32
-    br = 1 if fmt is _E2M1 else 128              # rows of a scale
+    shape, fmt, f32, xt = W1.shape, W1.dtype, torch.float32, x.dtype
+    lead = () if offsets is None else (shape[0],)
+    E, H = (lead[0] if lead else 1), shape[-2]
+    four = fmt is _E2M1
+    if not four:
+        fmt = torch.float8_e4m3fn
+    nh, nd = (H, D) if four else (-(-H // 128), -(-D // 128))           # rows of scales
     s = Shape(T, D, H, E, 1, 0, 0, _dt(x), 1)
     dev = x.get_device()
     args = (_shaped(W1, fmt, (*lead, H, _value_cols(D, fmt)), "weights W1", dev),
-            _shaped(W1_scale, e8, (*lead, -(-H // br), _scale_cols(D, fmt)), "W1_scale", dev),
-            _shaped_or_none(b1, f32, (*lead, H), "b1", dev),
+            _shaped(W1_scale, _E8M0, (*lead, nh, _scale_cols(D, fmt)), "W1_scale", dev),
+            None if b1 is None else _shaped(b1, f32, (*lead, H), "b1", dev),
             _shaped(W2, fmt, (*lead, D, _value_cols(H, fmt)), "weights W2", dev),
-            _shaped(W2_scale, e8, (*lead, -(-D // br), _scale_cols(H, fmt)), "W2_scale", dev),
-            _shaped_or_none(b2, f32, (*lead, D), "b2", dev),
-            _shaped_or_none(offsets, torch.int32, (E + 1,), "offsets", dev))
+            _shaped(W2_scale, _E8M0, (*lead, nd, _scale_cols(H, fmt)), "W2_scale", dev),
+            None if b2 is None else _shaped(b2, f32, (*lead, D), "b2", dev),
+            None if offsets is None else _shaped(offsets, torch.int32, (E + 1,), "offsets", dev))
     fa = _format(activations)
     xp, st = _ptr(x, dev), _queue(dev, stream)
     ws = _workspace(quantized_workspace_bytes(s), x, stream) if ws is None else ws
-    y = out if out is not None else torch.empty_like(x) if stream is None else _empty(x, (T, D), x.dtype, stream)
-    rc = lib().clearmoe_quantized_ffn_forward_ex(ctypes.byref(s), fa, _OUTS[fmt], xp, *args,
-                                                 _shaped(y, x.dtype, (T, D), "out", dev), _ptr(ws, dev), ws.numel(),
-                                                 st)
+    if out is None:
+        y = torch.empty_like(x) if stream is None else _empty(x, (T, D), xt, stream)
+        yp = y.data_ptr()
+    else:
+        y, yp = out, _shaped(out, xt, (T, D), "out", dev)
+    rc = lib().clearmoe_quantized_ffn_forward_ex(ctypes.byref(s), fa, 5 if four else 2, xp, *args, yp, _ptr(ws, dev),
+                                                 ws.numel(), st)
     _check(rc, "clearmoe_quantized_ffn_forward_ex")
     return y
 

@@ -599,12 +599,19 @@ int64_t q4_tiles(const Q8Desc& g, int bm, int bn) {
 //     1024 x 4096   64 x 128               13.9    14.1    16.1    46.0     178
 //                   128 x 128              19.3    19.6    20.1    34.2     131
 //                   128 x 256              30.2    30.5    31.0    35.2     119
-enum Q4Kernel { kQ4Rows, kQ4Small, kQ4Wide, kQ4Middle, kQ4Deep, kQ4Large };
+//   8-bit rows, float32
+//     1550 x 1200   64 x 64 (small)         6.9     7.5    24.9    77.2
+//                   64 x 128               ~9.8    10.2    13.5    41.1
+//                   64 x 128, two groups   ~8.5     9.0    17.8    57.0
+enum Q4Kernel { kQ4Rows, kQ4Small, kQ4Split, kQ4Wide, kQ4Middle, kQ4Deep, kQ4Large };
 template <int FA, int OUT>
 Q4Kernel q4_choose(const Q8Desc& g) {
     constexpr bool A4 = FA == kQ8E2M1, FLOAT = OUT == kQ8OutF32 || OUT == kQ8OutBf16;
     if (FLOAT && q4_tiles(g, 16, 16) <= 320) return kQ4Rows;
     if (OUT != kQ8OutE4M3 && q4_tiles(g, 64, 64) <= 256) return kQ4Small;
+    // (with a workgroup alone on its CU and a long sum, two groups of waves
+    // along k)
+    if (OUT != kQ8OutE4M3 && q4_tiles(g, 64, 128) <= 256 && g.K > (!A4 && OUT == kQ8OutF32 ? 512 : 2048)) return kQ4Split;
     if (q4_tiles(g, 64, 128) <= (A4 ? 400 : 512)) return kQ4Wide;
     if (OUT == kQ8OutF32) return A4 && g.K > 512 ? kQ4Deep : kQ4Middle;
     if (!A4) return q4_tiles(g, 128, 256) >= 384 ? kQ4Large : kQ4Middle;
@@ -619,8 +626,10 @@ hipError_t q4_launch(const Q8Desc& g, hipStream_t st) {
     const Q4Kernel kernel = q4_choose<FA, OUT>(g);
     if constexpr (F32 || BF16)
         if (kernel == kQ4Rows) return q4_rows<FA, typename std::conditional<F32, float, bf16_bits>::type>(g, st);
-    if constexpr (OUT != kQ8OutE4M3)
+    if constexpr (OUT != kQ8OutE4M3) {
         if (kernel == kQ4Small) return q4_tile<2, 2, 2, 1, 1, KS, FA, OUT, 2>(g, st);
+        if (kernel == kQ4Split) return q4_tile<2, 2, 2, 1, 2, KS, FA, OUT, 2>(g, st);
+    }
     if (kernel == kQ4Wide) return q4_tile<1, 2, 2, 1, 2, KS, FA, OUT, 2>(g, st);
     if constexpr (A4)
         if (kernel == kQ4Deep) return q4_tile<1, 2, 2, 2, 2, 256, FA, OUT, 2>(g, st);

@@ -19,18 +19,29 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // full-rate operations' time instead of gelu_erf's 20.  fc1 + GELU over many
 // rows is bound by this vector work (50432 x 3072 x 768: 199 us with gelu_erf,
 // 141 without any).  An infinite v gives NaN, as gelu_erf does.
-__device__ __forceinline__ float q8_gelu(float v) {
-    const float a = fabsf(v);
-    float p = __builtin_fmaf(a, -1.83535093e-06f, 6.16087855e-05f);
-    p = __builtin_fmaf(a, p, -9.3060248e-04f);
-    p = __builtin_fmaf(a, p, 8.50815862e-03f);
-    p = __builtin_fmaf(a, p, -5.39604758e-02f);
-    p = __builtin_fmaf(a, p, -4.58464246e-01f);
-    p = __builtin_fmaf(a, p, -1.15125091f);
-    p = __builtin_fmaf(a, p, -9.99995318e-01f);
-    float m;                                     // (fmaxf takes two instructions: it quiets NaN first)
-    asm("v_max_f32 %0, 0, %1" : "=v"(m) : "v"(v));
-    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), m);
+// Four at a time, step by step: an exponential's result may not be used by the
+// next instruction.
+__device__ __forceinline__ void q8_gelu4(float (&v)[4]) {
+    float p[4], m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = fabsf(v[i]);
+        p[i] = __builtin_fmaf(a, -1.83535093e-06f, 6.16087855e-05f);
+        p[i] = __builtin_fmaf(a, p[i], -9.3060248e-04f);
+        p[i] = __builtin_fmaf(a, p[i], 8.50815862e-03f);
+        p[i] = __builtin_fmaf(a, p[i], -5.39604758e-02f);
+        p[i] = __builtin_fmaf(a, p[i], -4.58464246e-01f);
+        p[i] = __builtin_fmaf(a, p[i], -1.15125091f);
+        p[i] = __builtin_fmaf(a, p[i], -9.99995318e-01f);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        // (fmaxf takes two instructions: it quiets NaN first)
+        asm("v_max_f32 %0, 0, %1" : "=v"(m[i]) : "v"(v[i]));
+        v[i] = __builtin_fmaf(-fabsf(v[i]), p[i], m[i]);
+    }
 }
 
 // Four floats over a scale -> four bytes (as q8_pack4, the division inside).
@@ -121,7 +132,14 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][j][v] = F32 ? gelu_erf(acc[i][j][v]) : q8_gelu(acc[i][j][v]);
+                for (int v = 0; v < 16; v += 4) {
+                    float x[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) x[c] = F32 ? gelu_erf(acc[i][j][v + c]) : acc[i][j][v + c];
+                    if (!F32) q8_gelu4(x);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[i][j][v + c] = x[c];
+                }
     float mx[TM];
     if constexpr (!F32 && !BF16 && !E2M1) {
         // Bytes past N are zeros whatever the row holds (their sums are zeros

@@ -467,7 +467,7 @@ int clearmoe_rms_norm(const clearmoe_norm* norm, const void* x, const void* resi
  *              is quantised to 4 bits, ldc a multiple of 32.
  *   sums       of 4-bit A hold all of a product; of e4m3 A as above (1.2e-5 of
  *              the result's norm is cut but for F32 results).
- *   a launch   holds (ceil(M / 128) + groups) ceil(N / 128) at most 2^24 - 8. */
+ *   a launch   holds (ceil(M / 128) + 2 groups) ceil(N / 128) at most 2^24 - 32. */
 typedef struct {
     int64_t M;
     int32_t N, K;

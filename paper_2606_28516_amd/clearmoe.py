@@ -255,7 +255,7 @@ def _empty(x: torch.Tensor, shape: tuple, dtype, stream, kept: bool = True) -> t
     the same stream only.  kept: the caller gets it, and may let go of it while
     the current stream still reads it."""
     if stream is None:
-        return x.new_empty(shape, dtype=dtype)
+        return x.new_empty(*shape, dtype=dtype)  # (a tuple in one piece costs more)
     with torch.cuda.stream(stream):
         t = x.new_empty(shape, dtype=dtype)
     if kept and t.is_cuda:
@@ -652,7 +652,8 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, out_dtype=None,
     plain = x if stream is None and x.is_contiguous() else None         # (empty_like costs less)
     if sum_out is None and residual is not None:
         sum_out = torch.empty_like(x) if plain is not None else _empty(x, (rows, cols), xt, stream)
-    y = out if out is not None else torch.empty_like(x) if plain is not None and not byte else _empty(x, yshape, ot, stream)
+    y = (out if out is not None else torch.empty_like(x, dtype=ot) if plain is not None and yshape == shape
+         else _empty(x, yshape, ot, stream))
     ys = _empty(x, (rows, _scale_cols(cols)), _E8M0, stream) if byte else None
     ld = [0 if t is None or t.is_contiguous() else _row_stride(t, what)
           for t, what in ((x, "rows of x"), (residual, "rows of residual"), (sum_out, "rows of sum_out"), (y, "rows of out"))]

@@ -603,27 +603,28 @@ int64_t q4_tiles(const Q8Desc& g, int bm, int bn) {
 //     1550 x 1200   64 x 64 (small)         6.9     7.5    24.9    77.2
 //                   64 x 128               ~9.8    10.2    13.5    41.1
 //                   64 x 128, two groups   ~8.5     9.0    17.8    57.0
-enum Q4Kernel { kQ4Rows, kQ4Small, kQ4Split, kQ4Wide, kQ4Middle, kQ4Deep, kQ4Large };
-template <int FA, int OUT>
 Q4Kernel q4_choose(const Q8Desc& g) {
-    constexpr bool A4 = FA == kQ8E2M1, FLOAT = OUT == kQ8OutF32 || OUT == kQ8OutBf16;
-    if (FLOAT && q4_tiles(g, 16, 16) <= 320) return kQ4Rows;
-    if (OUT != kQ8OutE4M3 && q4_tiles(g, 64, 64) <= 256) return kQ4Small;
+    const bool a4 = g.fa == kQ8E2M1, f32 = g.out == kQ8OutF32, floats = f32 || g.out == kQ8OutBf16;
+    if (floats && q4_tiles(g, 16, 16) <= 320) return kQ4Rows;
+    // an 8-bit result's block needs 128 columns of a tile and all its waves
+    const bool parts = g.out != kQ8OutE4M3;
+    if (parts && q4_tiles(g, 64, 64) <= 256) return kQ4Small;
+    const int64_t wide = q4_tiles(g, 64, 128);
     // (with a workgroup alone on its CU and a long sum, two groups of waves
     // along k)
-    if (OUT != kQ8OutE4M3 && q4_tiles(g, 64, 128) <= 256 && g.K > (!A4 && OUT == kQ8OutF32 ? 512 : 2048)) return kQ4Split;
-    if (q4_tiles(g, 64, 128) <= (A4 ? 400 : 512)) return kQ4Wide;
-    if (OUT == kQ8OutF32) return A4 && g.K > 512 ? kQ4Deep : kQ4Middle;
-    if (!A4) return q4_tiles(g, 128, 256) >= 384 ? kQ4Large : kQ4Middle;
+    if (parts && wide <= 256 && g.K > (f32 && !a4 ? 512 : 2048)) return kQ4Split;
+    if (wide <= (a4 ? 400 : 512)) return kQ4Wide;
+    if (f32) return a4 && g.K > 512 ? kQ4Deep : kQ4Middle;
+    if (!a4) return q4_tiles(g, 128, 256) >= 384 ? kQ4Large : kQ4Middle;
     if (g.K <= 512) return kQ4Middle;
-    return (FLOAT ? q4_tiles(g, 256, 256) >= 240 : q4_tiles(g, 128, 256) >= 400) ? kQ4Large : kQ4Deep;
+    return (floats ? q4_tiles(g, 256, 256) >= 240 : q4_tiles(g, 128, 256) >= 400) ? kQ4Large : kQ4Deep;
 }
 
 template <int FA, int OUT>
 hipError_t q4_launch(const Q8Desc& g, hipStream_t st) {
     constexpr bool A4 = FA == kQ8E2M1, F32 = OUT == kQ8OutF32, BF16 = OUT == kQ8OutBf16;
     constexpr int KS = A4 ? 256 : 128;
-    const Q4Kernel kernel = q4_choose<FA, OUT>(g);
+    const Q4Kernel kernel = q4_choose(g);
     if constexpr (F32 || BF16)
         if (kernel == kQ4Rows) return q4_rows<FA, typename std::conditional<F32, float, bf16_bits>::type>(g, st);
     if constexpr (OUT != kQ8OutE4M3) {
@@ -661,10 +662,12 @@ hipError_t q4_few_out(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStr
 
 }  // namespace
 
+Q4Kernel q4_kernel(const Q8Desc& g) { return q4_choose(g); }
 bool q4_launch_fits(int64_t M, int N, int groups) {
-    // 128 x 128 tiles over 256 threads at the least (smaller ones are for few
-    // of them; the grid is rounded up to whole XCDs)
-    return ((M + 127) / 128 + groups) * q8_blocks(N) <= (int64_t{1} << 32) / 256 - kGbXcds;
+    // many rows take 128 x 128 tiles over 256 threads at the least, or 256 x 256
+    // over 512, for which a group's half tile more counts twice (the grid is
+    // rounded up to whole XCDs)
+    return ((M + 127) / 128 + 2 * static_cast<int64_t>(groups)) * q8_blocks(N) <= (int64_t{1} << 32) / 256 - 4 * kGbXcds;
 }
 bool q4_few_supported(int64_t M, int64_t K) {
     const int64_t rows = M < 16 ? M : 16;

@@ -209,6 +209,11 @@ hipError_t launch_q8_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hip
 // stride of bytes in bytes: a row of B has q4_cols(K) of them, SB
 // q4_scale_cols(K) for each of N, a row of e2m1 results ldc.
 hipError_t launch_gemm_q4(const Q8Desc& g, hipStream_t st);
+// The kernel that a product takes: 16 x 16 tiles, 64 x 64, 64 x 128 (split: by
+// two groups of waves along k), 128 x 128 (deep: 256 of k a stage), or 256 x
+// 256 (4-bit rows to bfloat16) and 128 x 256.
+enum Q4Kernel { kQ4Rows, kQ4Small, kQ4Split, kQ4Wide, kQ4Middle, kQ4Deep, kQ4Large };
+Q4Kernel q4_kernel(const Q8Desc& g);
 // Whether the product fits one launch.
 bool q4_launch_fits(int64_t M, int N, int groups);
 // As launch_q8_few, the rows quantised to fa.

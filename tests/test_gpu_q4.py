@@ -191,7 +191,7 @@ def _check_product(M, N, K, E=0, offsets=None, fa=E4M3, out=BF16, bias=True, gel
 
 ROWS = [E4M3, E2M1]
 MORE = [(1, 1, 32), (64, 128, 512), (65, 129, 544), (70, 64, 1024), (300, 200, 1056), (20, 500, 4128), (1, 8, 65536),
-        (1000, 1540, 1200), (500, 1030, 2112)]
+        (1000, 1540, 1200), (1000, 1030, 2112), (1000, 1030, 176)]
 
 
 @pytest.mark.parametrize("out", [BF16, F32, E4M3, E2M1])
@@ -208,13 +208,16 @@ def test_product_groups(M, N, K, offsets, fa, out):
     _check_product(M, N, K, E=len(offsets) - 1, offsets=offsets, fa=fa, out=out, gelu=N % 16 == 0)
 
 
-@pytest.mark.parametrize("M,N,K,offsets,fa,out", [
+MANY = [
     (8200, 1990, 544, None, E2M1, BF16), (6500, 1830, 576, None, E2M1, E2M1), (6500, 1830, 576, None, E2M1, E4M3),
     (3000, 1300, 640, None, E2M1, F32), (3000, 1300, 640, None, E2M1, BF16), (3000, 1300, 640, None, E2M1, E2M1),
     (3000, 1300, 640, None, E2M1, E4M3), (6500, 1830, 160, None, E4M3, BF16), (6500, 1830, 160, None, E4M3, E4M3),
     (6500, 1830, 160, None, E4M3, E2M1), (9000, 1900, 544, [0, 5, 4000, 4001, 9000], E2M1, BF16),
     (7000, 1900, 544, [9, 3000, 3000, 6995], E2M1, E2M1), (7000, 1900, 160, [9, 3000, 3000, 6995], E4M3, E4M3),
-    (3000, 1300, 640, [7, 1000, 1000, 2900], E2M1, F32)])
+    (3000, 1300, 640, [7, 1000, 1000, 2900], E2M1, F32)]
+
+
+@pytest.mark.parametrize("M,N,K,offsets,fa,out", MANY)
 def test_product_of_many_rows(M, N, K, offsets, fa, out):
     """The largest tiles, and those for a long k."""
     _check_product(M, N, K, E=len(offsets) - 1 if offsets else 0, offsets=offsets, fa=fa, out=out, gelu=N % 20 == 0)

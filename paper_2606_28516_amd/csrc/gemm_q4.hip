@@ -194,15 +194,13 @@ __global__ __launch_bounds__(512) void k_q4_few(Q8Desc g, const TA* A, int K0, i
             uint32_t w = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w = max(w, q4_mag(f[i]));
-            w = max(w, static_cast<uint32_t>(__shfl_xor(static_cast<int>(w), 1)));
-            w = max(w, static_cast<uint32_t>(__shfl_xor(static_cast<int>(w), 2)));
+            w = max(w, static_cast<uint32_t>(q8_partner<1>(static_cast<int>(w))));
+            w = max(w, static_cast<uint32_t>(q8_partner<2>(static_cast<int>(w))));
             const int e = q4_exponent(w);
             *reinterpret_cast<uint32_t*>(s_a + m * pitch + blk * 64 + sub * 4) = q4_pack8(f, e);
             if (sub % 4 == 0) s_sa[m * spitch + blk * 4 + sub / 4] = static_cast<unsigned char>(e + kQ8One);
         } else {
-            float a = q8_mag8(f);
-#pragma unroll
-            for (int s = kQ8Lanes / 2; s > 0; s >>= 1) a = fmaxf(a, __shfl_xor(a, s));
+            const float a = q8_max16(q8_mag8(f));
             const int e = q8_exponent(__float_as_uint(a), q8_top_exp(kQ8E4M3));
             *reinterpret_cast<uint2*>(s_a + m * pitch + blk * kQ8Block + sub * 8) =
                 q8_pack8<kQ8E4M3>(f, q8_two_to(-e));

@@ -170,9 +170,7 @@ __global__ __launch_bounds__(512) void k_q8_few(Q8Desc g, const TA* A, int K0, i
         const int m = u / nk, blk = u - m * nk, sub = tid % kQ8Lanes;
         float f[8];
         q8_load8(A + (t.m_lo + m) * K0, blk * kQ8Block + sub * 8, K0, f);
-        float a = q8_mag8(f);
-#pragma unroll
-        for (int s = kQ8Lanes / 2; s > 0; s >>= 1) a = fmaxf(a, __shfl_xor(a, s));
+        const float a = q8_max16(q8_mag8(f));
         const int e = q8_exponent(__float_as_uint(a), q8_top_exp(kQ8E4M3));
         *reinterpret_cast<uint2*>(s_a + m * pitch + blk * kQ8Block + sub * 8) = q8_pack8<kQ8E4M3>(f, q8_two_to(-e));
         if (sub == 0) s_sa[m * nk + blk] = static_cast<unsigned char>(e + kQ8One);

@@ -77,6 +77,27 @@ __device__ __forceinline__ uint32_t q8_pack4(float a, float b, float c, float d)
     return static_cast<uint32_t>(v);
 }
 
+// The value of a lane's partner in its row of 16 lanes: the steps of a
+// butterfly over 2, 4, 8 and 16 lanes (the last two mirror the halves, which is
+// as good once the smaller groups agree).  In the vector unit, without the LDS
+// that a shuffle takes.
+template <int STEP>
+__device__ __forceinline__ int q8_partner(int v) {
+    constexpr int CTRL = STEP == 1 ? 0xb1 : STEP == 2 ? 0x4e : STEP == 4 ? 0x141 : 0x140;
+    return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
+template <int STEP>
+__device__ __forceinline__ float q8_partner(float v) {
+    return __int_as_float(q8_partner<STEP>(__float_as_int(v)));
+}
+// The largest of 16 lanes.
+__device__ __forceinline__ float q8_max16(float m) {
+    m = fmaxf(m, q8_partner<1>(m));
+    m = fmaxf(m, q8_partner<2>(m));
+    m = fmaxf(m, q8_partner<4>(m));
+    return fmaxf(m, q8_partner<8>(m));
+}
+
 // A lane's share of a 128-column block when 16 lanes quantise it: columns
 // [c, c + 8) of a row, zeros from n on.  (A piece may start at any element:
 // the hardware loads it all the same.)

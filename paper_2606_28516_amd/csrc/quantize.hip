@@ -25,9 +25,7 @@ __global__ __launch_bounds__(kThreads) void k_quantize_rows(const T* x, int64_t 
     const int64_t row = b / blocks, blk = b - row * blocks, c = blk * kQ8Block + sub * 8;
     float f[8];
     q8_load8(x + row * ldx, c, cols, f);
-    float m = q8_mag8(f);
-#pragma unroll
-    for (int s = kLanes / 2; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
+    const float m = q8_max16(q8_mag8(f));
     const int e = q8_exponent(__float_as_uint(m), q8_top_exp(FMT));
     if (c < vcols) *reinterpret_cast<uint2*>(v + row * vcols + c) = q8_pack8<FMT>(f, q8_two_to(-e));
     if (sub == 0) {
@@ -53,14 +51,14 @@ __global__ __launch_bounds__(kThreads) void k_quantize4(const T* x, int64_t ldx,
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, q4_mag(f[i]));
-    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 1)));
-    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 2)));
+    m = max(m, static_cast<uint32_t>(q8_partner<1>(static_cast<int>(m))));
+    m = max(m, static_cast<uint32_t>(q8_partner<2>(static_cast<int>(m))));
     const int e = q4_exponent(m);
     if (c / 2 < vcols) *reinterpret_cast<uint32_t*>(v + row * vcols + c / 2) = q4_pack8(f, e);
     // (blocks past the last have no columns: zeros, the scale 1)
     uint32_t w = static_cast<uint32_t>(e + kQ8One) << (8 * (sub / 4));
-    w |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(w), 4));
-    w |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(w), 8));
+    w |= static_cast<uint32_t>(q8_partner<4>(static_cast<int>(w)));
+    w |= static_cast<uint32_t>(q8_partner<8>(static_cast<int>(w)));
     if (sub == 0) reinterpret_cast<uint32_t*>(scale)[row * units + unit] = w;
 }
 

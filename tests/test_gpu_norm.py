@@ -60,7 +60,7 @@ def _inputs(rows, cols, dtype, seed):
 
 WIDTHS = [(1, 1), (3, 7), (5, 8), (2, 16), (9, 127), (4, 128), (130, 129), (1, 768), (257, 384), (64, 511), (6, 512),
           (7, 513), (33, 1000), (5, 1024), (5, 1025), (3, 2048), (3, 2049), (4, 4096), (2, 4099), (3, 8192), (2, 8200),
-          (2, 16384), (2, 16400), (1, 32768), (2, 33001), (1, 65536), (2, 65535)]
+          (2, 16384), (2, 16400), (1, 32768), (2, 33001), (1, 65536), (2, 65535), (1030, 700), (1030, 1000), (1025, 8000), (1027, 4100)]
 
 
 @pytest.mark.parametrize("dtype,out", [(BF16, BF16), (F32, F32), (BF16, E4M3), (F32, E4M3), (BF16, E5M2), (F32, E5M2)])

@@ -21,18 +21,27 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // 141 without any).  An infinite v gives NaN, as gelu_erf does.
 // Four at a time, step by step: an exponential's result may not be used by the
 // next instruction.
+// For results of 4 bits (E2M1) P(0) is -1 itself, and P off by 5.7e-6 at most:
+// sums of 4-bit products lie on a coarse grid, so the halves that GELU makes of
+// small ones (below 2^-20) are often ties of the result's grid, or six times a
+// power of two, and must not be moved off them.
+template <bool E2M1>
 __device__ __forceinline__ void q8_gelu4(float (&v)[4]) {
+    constexpr float P[8] = {E2M1 ? -1.0f : -9.99995318e-01f,
+                            E2M1 ? -1.15121424f : -1.15125091f,
+                            E2M1 ? -4.58541691e-01f : -4.58464246e-01f,
+                            E2M1 ? -5.38909398e-02f : -5.39604758e-02f,
+                            E2M1 ? 8.4768841e-03f : 8.50815862e-03f,
+                            E2M1 ? -9.23200278e-04f : -9.3060248e-04f,
+                            E2M1 ? 6.07283946e-05f : 6.16087855e-05f,
+                            E2M1 ? -1.7939027e-06f : -1.83535093e-06f};
     float p[4], m[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float a = fabsf(v[i]);
-        p[i] = __builtin_fmaf(a, -1.83535093e-06f, 6.16087855e-05f);
-        p[i] = __builtin_fmaf(a, p[i], -9.3060248e-04f);
-        p[i] = __builtin_fmaf(a, p[i], 8.50815862e-03f);
-        p[i] = __builtin_fmaf(a, p[i], -5.39604758e-02f);
-        p[i] = __builtin_fmaf(a, p[i], -4.58464246e-01f);
-        p[i] = __builtin_fmaf(a, p[i], -1.15125091f);
-        p[i] = __builtin_fmaf(a, p[i], -9.99995318e-01f);
+        p[i] = P[7];
+#pragma unroll
+        for (int k = 6; k >= 0; --k) p[i] = __builtin_fmaf(a, p[i], P[k]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
@@ -136,7 +145,7 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
                     float x[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) x[c] = F32 ? gelu_erf(acc[i][j][v + c]) : acc[i][j][v + c];
-                    if (!F32) q8_gelu4(x);
+                    if (!F32) q8_gelu4<E2M1>(x);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) acc[i][j][v + c] = x[c];
                 }

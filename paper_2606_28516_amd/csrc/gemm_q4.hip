@@ -296,7 +296,7 @@ struct Q4Rows {
 // groups take the pieces of 512 in turn and their sums are added at the end.
 //
 // Measured on an MI355X, calls in a row: 4-bit rows 8192 x 8192 x 8192 to
-// bfloat16 276 us (3990 TFLOP/s), 50432 x 1024 x 4096 136, 50432 x 4096 x 1024
+// bfloat16 276 us (3990 TFLOP/s), 50432 x 1024 x 4096 140, 50432 x 4096 x 1024
 // with GELU to 4 bits 190; 8-bit rows 420 (2600), 195, and to e4m3 230.  Bounds:
 // the large one takes 168 us without its matrix instructions (what 256 CUs take
 // from the L2s, 12.5 TB/s) and 211 without its loads (the card's power: these
@@ -632,6 +632,24 @@ Q4Kernel q4_choose(const Q8Desc& g) {
     return (floats ? q4_tiles(g, 256, 256) >= 240 : q4_tiles(g, 128, 256) >= 400) ? kQ4Large : kQ4Deep;
 }
 
+// 256 x 256 tiles, one a CU: a few more than the CUs have in whole rounds take
+// a round of their own, so the rows past the whole rounds become a product of
+// their own with the tiles that suit them, up to a quarter of a round or, with
+// a sum long enough to hide the second launch, half of one.  One launch and two,
+// us on an MI355X, N = 1024:
+//   tiles / 256     1.02          1.12          1.25          1.5           3.08
+//   K  544      24.1  19.9    23.8  21.1    23.7  22.9    24.3  25.8    46.9  43.7
+//   K 2048      38.5  30.1    37.8  32.9    38.3  35.2    40.4  40.2    82.0  76.1
+//   K 4096      65.1  48.3    64.8  53.0    65.3  58.0    68.3  66.2     140   127
+// Tiles of 128 x 256, two a CU, win at 1.02 only (79 -> 71) and lose from 1.25 on
+// (81 -> 85); a group's rows are not known here.
+int64_t q4_whole(const Q8Desc& g) {
+    if (q4_choose(g) != kQ4Large || g.fa != kQ8E2M1 || g.out != kQ8OutBf16 || g.seg_offsets != nullptr) return g.M;
+    const int64_t nt = (g.N + 255) / 256, tiles = (g.M + 255) / 256 * nt;
+    const int64_t whole = tiles / 256 * 256 / nt, rest = tiles - whole * nt;      // rows of tiles, tiles
+    return whole > 0 && rest > 0 && rest <= (g.K >= 2048 ? 128 : 64) ? whole * 256 : g.M;
+}
+
 template <int FA, int OUT>
 hipError_t q4_launch(const Q8Desc& g, hipStream_t st) {
     constexpr bool A4 = FA == kQ8E2M1, F32 = OUT == kQ8OutF32, BF16 = OUT == kQ8OutBf16;
@@ -675,6 +693,7 @@ hipError_t q4_few_out(const Q8Desc& g, const void* A, bool a_f32, int K0, hipStr
 }  // namespace
 
 Q4Kernel q4_kernel(const Q8Desc& g) { return q4_choose(g); }
+int64_t q4_whole_rows(const Q8Desc& g) { return q4_whole(g); }
 bool q4_launch_fits(int64_t M, int N, int groups) {
     // many rows take 128 x 128 tiles over 256 threads at the least, or 256 x 256
     // over 512, for which a group's half tile more counts twice (the grid is
@@ -692,6 +711,16 @@ hipError_t launch_q4_few(const Q8Desc& g, const void* A, bool a_f32, int K0, hip
 
 hipError_t launch_gemm_q4(const Q8Desc& g, hipStream_t st) {
     if (g.M == 0) return hipSuccess;
+    if (const int64_t rows = q4_whole(g); rows < g.M) {
+        Q8Desc first = g, rest = g;              // (bfloat16)
+        first.M = rows;
+        rest.M -= rows;
+        rest.A += rows * g.lda;
+        rest.SA += rows * g.sa_ld;
+        rest.C = static_cast<bf16_bits*>(g.C) + rows * g.ldc;
+        const hipError_t e = q4_out<kQ8E2M1>(first, st);
+        return e != hipSuccess ? e : q4_out<kQ8E2M1>(rest, st);
+    }
     return g.fa == kQ8E2M1 ? q4_out<kQ8E2M1>(g, st) : q4_out<kQ8E4M3>(g, st);
 }
 

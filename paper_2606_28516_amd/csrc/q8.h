@@ -235,6 +235,8 @@ hipError_t launch_gemm_q4(const Q8Desc& g, hipStream_t st);
 // 256 (4-bit rows to bfloat16) and 128 x 256.
 enum Q4Kernel { kQ4Rows, kQ4Small, kQ4Split, kQ4Wide, kQ4Middle, kQ4Deep, kQ4Large };
 Q4Kernel q4_kernel(const Q8Desc& g);
+// The rows that a first launch takes; the others follow in a second one.
+int64_t q4_whole_rows(const Q8Desc& g);
 // Whether the product fits one launch.
 bool q4_launch_fits(int64_t M, int N, int groups);
 // As launch_q8_few, the rows quantised to fa.

@@ -66,6 +66,32 @@ static void launch() {
                     }
 }
 
+// Products in two launches: whole tiles of rows first, neither part cut again,
+// and each row in one of them.
+static void rounds() {
+    int cut = 0;
+    for (int fa : {kQ8E4M3, kQ8E2M1})
+        for (int out : {kQ8OutF32, kQ8OutBf16, kQ8OutE4M3, kQ8OutE2M1})
+            for (int K : {32, 544, 2048, 65536})
+                for (int groups : {0, 3})
+                    for (int N : {1, 256, 384, 1000, 4096, 65536})
+                        for (int64_t M = 1; M < int64_t{1} << 31; M += M / 7 + 1) {
+                            Q8Desc g = desc(M, N, K, groups, fa, out);
+                            const int64_t rows = q4_whole_rows(g);
+                            if (rows == M) continue;
+                            ++cut;
+                            expect(fa == kQ8E2M1 && out == kQ8OutBf16 && groups == 0, "cut", M, N);
+                            expect(rows > 0 && rows < M && rows % 256 == 0, "rows", M, rows);
+                            expect((M - rows + 255) / 256 * ((N + 255) / 256) <= 128, "the rest", M, rows);
+                            g.M = rows;
+                            expect(q4_whole_rows(g) == rows && q4_launch_fits(rows, N, 0) >= q4_launch_fits(M, N, 0),
+                                   "first", M, rows);
+                            g.M = M - rows;
+                            expect(q4_whole_rows(g) == g.M, "rest", M, rows);
+                        }
+    expect(cut > 100, "cut products", cut, 0);
+}
+
 // The kernel of each product M N K groups fa out (as q8.h numbers them).
 static void kernels(int n, char** v) {
     for (int i = 0; i + 5 < n; i += 6)
@@ -76,6 +102,12 @@ static void kernels(int n, char** v) {
 int main(int argc, char** argv) {
     if (argc < 2) return 2;
     if (std::strcmp(argv[1], "launch") == 0) launch();
+    else if (std::strcmp(argv[1], "rounds") == 0) rounds();
+    else if (std::strcmp(argv[1], "whole") == 0)
+        for (int i = 2; i + 2 < argc; i += 3)
+            std::printf("%ld\n", static_cast<long>(q4_whole_rows(
+                                     desc(std::atol(argv[i]), std::atoi(argv[i + 1]), std::atoi(argv[i + 2]), 0, kQ8E2M1,
+                                          kQ8OutBf16))));
     else if (std::strcmp(argv[1], "kernels") == 0) kernels(argc - 2, argv + 2);
     else return 2;
     return g_bad != 0;

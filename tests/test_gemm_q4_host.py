@@ -23,8 +23,9 @@ def program(tmp_path_factory):
     return out
 
 
-def test_launch(program):
-    r = subprocess.run([program, "launch"], capture_output=True, text=True, timeout=60)
+@pytest.mark.parametrize("what", ["launch", "rounds"])
+def test_launch(program, what):
+    r = subprocess.run([program, what], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, r.stdout + r.stderr
 
 
@@ -48,3 +49,9 @@ def test_gpu_sizes_cover_every_kernel(program, fa, out):
     names = subprocess.run([program, "kernels", *args], capture_output=True, text=True, check=True,
                            timeout=60).stdout.split()
     assert set(names) == ALL[fa, out]
+
+
+def test_gpu_sizes_of_two_launches(program):
+    args = [str(v) for M, N, K, _ in gpu.ROUNDS for v in (M, N, K)]
+    rows = subprocess.run([program, "whole", *args], capture_output=True, text=True, check=True, timeout=60).stdout.split()
+    assert [int(r) for r in rows] == [w for *_, w in gpu.ROUNDS]

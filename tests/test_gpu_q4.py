@@ -347,6 +347,35 @@ def test_product_row_strides(M, fa, out):
         assert torch.equal(cs, want[1].view(torch.uint8))
 
 
+# (M, N, K) whose rows after the first `whole` are a launch of their own
+ROUNDS = [(13100, 1270, 544, 13056), (8200, 2000, 1024, 8192), (600, 21800, 2080, 512), (17000, 1024, 2048, 16384),
+          (20480, 1024, 2048, 16384)]
+
+
+@pytest.mark.parametrize("M,N,K,whole", ROUNDS)
+def test_product_of_a_few_more_rows_than_whole_rounds(M, N, K, whole):
+    """Rows inside wider arrays, results that begin at any element: as the two
+    parts' own products; bytes around them stay as they were."""
+    g = torch.Generator(device="cuda").manual_seed(19)
+    a, sa = cm.quantize(torch.randn(M, K, device="cuda", generator=g), E2M1)
+    b, sb = cm.quantize(torch.randn(N, K, device="cuda", generator=g), E2M1)
+    bias = torch.randn(N, device="cuda", generator=g)
+    ptr = lambda t: ctypes.c_void_p(t.data_ptr())
+    wide = torch.full((M, K // 2 + 48), 0x7e, dtype=torch.uint8, device="cuda")
+    wide[:, :K // 2] = a.view(torch.uint8)
+    parts = [cm.quantized_gemm(a[lo:hi].contiguous(), sa[lo:hi].contiguous(), b, sb, bias=bias, gelu=True, out_dtype=BF16)
+             for lo, hi in ((0, whole), (whole, M))]
+    for at, ldc in ((0, N), (1, N + 9), (8, (N + 7) // 8 * 8 + 16)):
+        flat = torch.full((at + M * ldc + 8,), 7.5, dtype=BF16, device="cuda")
+        p = cm.Product(M, N, K, 0, 5, 5, cm.BF16, 1, 0, K + 96, ldc)
+        rc = cm.lib().clearmoe_quantized_gemm(ctypes.byref(p), ptr(wide), ptr(sa), ptr(b), ptr(sb), ptr(bias), None,
+                                              ptr(flat[at:]), None, cm._stream(None))
+        assert rc == 0
+        c = flat[at:at + M * ldc].view(M, ldc)
+        assert torch.equal(c[:whole, :N], parts[0]) and torch.equal(c[whole:, :N], parts[1])
+        assert (c[:, N:] == 7.5).all() and (flat[:at] == 7.5).all() and (flat[at + M * ldc:] == 7.5).all()
+
+
 def test_product_unaligned_results():
     """Float results at any element, of any width."""
     g = _gen(18)

@@ -600,6 +600,14 @@ int64_t q4_tiles(const Q8Desc& g, int bm, int bn) {
 //                   128 x 128, 128 of k    15.8    16.0    16.7    28.7     109
 //                   128 x 128, 256 of k    12.9    13.2    13.9    24.1    89.6
 //                   256 x 256              26.6    28.0    28.4    31.1    77.8
+//   by tiles of 128 x 128 (256 x 256: a quarter), eight groups from 1056 on (with the second k)
+//                                              320     512     600     752    1056    1360    2128    3200
+//     K 576, 544    128 x 128, 128 of k          8.3     9.5    10.5    11.4    18.5    20.8    29.0    40.9
+//                   128 x 128, 256 of k          8.6     9.7    12.5    12.9    19.5    22.9    31.6    43.8
+//                   256 x 256                   10.9    11.7    11.8    12.4    24.1    24.1    35.8    47.7
+//     K 2048, 4096  128 x 128, 128 of k         13.6    16.2    19.6    22.1    62.3    76.8     114     168
+//                   128 x 128, 256 of k         12.4    14.6    19.7    20.7   57.3    65.7    99.9     141
+//                   256 x 256                   17.5    19.0    19.3    20.0   66.8    67.6     103     141
 //   the same, GELU, to 4 bits
 //     4096 x 1024   128 x 128, 256 of k     7.3     7.6    10.1    34.3     132
 //                   128 x 256              11.3    11.5    12.5    32.4     123
@@ -628,8 +636,21 @@ Q4Kernel q4_choose(const Q8Desc& g) {
     if (wide <= (a4 ? 400 : 512)) return kQ4Wide;
     if (f32) return a4 && g.K > 512 ? kQ4Deep : kQ4Middle;
     if (!a4) return q4_tiles(g, 128, 256) >= 384 ? kQ4Large : kQ4Middle;
+    // 4-bit rows: a CU holds three workgroups of 128 x 128 with stages of 128 of
+    // k, two with 256 or of 128 x 256, one of 256 x 256; what runs in one round
+    // of the chip less wins, but a long sum wants the larger tile or stage
     if (g.K <= 512) return kQ4Middle;
-    return (floats ? q4_tiles(g, 256, 256) >= 240 : q4_tiles(g, 128, 256) >= 400) ? kQ4Large : kQ4Deep;
+    const int64_t tiles = q4_tiles(g, 128, 128);
+    if (tiles <= 512) return kQ4Deep;
+    if (tiles <= 768 && g.K < 2048) return kQ4Middle;
+    if (!floats) return q4_tiles(g, 128, 256) >= 400 ? kQ4Large : kQ4Deep;
+    const int64_t large = q4_tiles(g, 256, 256), rounds = (large + 255) / 256;
+    if (rounds == 1) return kQ4Large;
+    if (g.K <= 640) return kQ4Middle;
+    // three quarters of the rounds' places taken, or the last round's rows in a
+    // launch of their own (q4_whole)
+    if (large * 4 >= rounds * 768 || (g.seg_offsets == nullptr && (g.K >= 2048 || rounds > 2))) return kQ4Large;
+    return kQ4Deep;
 }
 
 // 256 x 256 tiles, one a CU: a few more than the CUs have in whole rounds take

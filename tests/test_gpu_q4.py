@@ -214,7 +214,9 @@ MANY = [
     (3000, 1300, 640, None, E2M1, E4M3), (6500, 1830, 160, None, E4M3, BF16), (6500, 1830, 160, None, E4M3, E4M3),
     (6500, 1830, 160, None, E4M3, E2M1), (9000, 1900, 544, [0, 5, 4000, 4001, 9000], E2M1, BF16),
     (7000, 1900, 544, [9, 3000, 3000, 6995], E2M1, E2M1), (7000, 1900, 160, [9, 3000, 3000, 6995], E4M3, E4M3),
-    (3000, 1300, 640, [7, 1000, 1000, 2900], E2M1, F32)]
+    (3000, 1300, 640, [7, 1000, 1000, 2900], E2M1, F32), (6600, 1990, 672, None, E2M1, BF16),
+    (6400, 1900, 672, [0, 5, 4000, 4001, 6400], E2M1, BF16), (9000, 1500, 544, None, E2M1, E2M1),
+    (9000, 1500, 544, None, E2M1, E4M3)]
 
 
 @pytest.mark.parametrize("M,N,K,offsets,fa,out", MANY)
@@ -348,7 +350,7 @@ def test_product_row_strides(M, fa, out):
 
 
 # (M, N, K) whose rows after the first `whole` are a launch of their own
-ROUNDS = [(13100, 1270, 544, 13056), (8200, 2000, 1024, 8192), (600, 21800, 2080, 512), (17000, 1024, 2048, 16384),
+ROUNDS = [(13100, 1270, 2080, 13056), (16500, 2000, 1024, 16384), (600, 21800, 2080, 512), (17000, 1024, 2048, 16384),
           (20480, 1024, 2048, 16384)]
 
 

@@ -38,7 +38,7 @@ def _operand(g, rows, K, fmt, exponents, tiny=False):
 # 16 x 16 tiles, 64 x 64, 64 x 128, two groups along k, 128 x 128 of both
 # stages, the largest
 SIZES = [(5, 40, 400), (300, 390, 400), (300, 1550, 400), (1000, 1030, 2112), (4200, 1550, 400), (3000, 1300, 640),
-         (8200, 1990, 544)]
+         (6600, 1990, 672)]
 
 
 def _check(M, N, K, fa, out, ea, eb, tiny=False):

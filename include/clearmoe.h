@@ -461,12 +461,11 @@ int clearmoe_rms_norm(const clearmoe_norm* norm, const void* x, const void* resi
  * 4-bit B (b_format CLEARMOE_E2M1): [N, K] or [E, N, K] with a scale for each 32
  * values of a row, so b_scale is [N, .] or [E, N, .].
  *   a_format   CLEARMOE_E4M3, or CLEARMOE_E2M1: then K, lda are multiples of 32,
- *              and products run at twice the rate.  (With e4m3 rows of a K that
- *              is no multiple of 32, b's rows are padded further than a's.)
+ *              and a large product takes half the time.  (With e4m3 rows of a K
+ *              that is no multiple of 32, b's rows are padded further than a's.)
  *   out        CLEARMOE_F32, CLEARMOE_BF16, CLEARMOE_E4M3, or CLEARMOE_E2M1: C
  *              is quantised to 4 bits, ldc a multiple of 32.
- *   sums       of 4-bit A hold all of a product; of e4m3 A as above (1.2e-5 of
- *              the result's norm is cut but for F32 results).
+ *   sums       hold all of a product, whatever A and the result are.
  *   a launch   holds (ceil(M / 128) + 2 groups) ceil(N / 128) at most 2^24 - 32. */
 typedef struct {
     int64_t M;

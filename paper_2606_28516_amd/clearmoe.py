@@ -674,13 +674,13 @@ def quantized_gemm(a, a_scale, b, b_scale, bias=None, gelu: bool = False, offset
     b [E, N, K] for the rows of each expert (rows outside all groups are left
     as out had them; their scales, of an 8-bit result, are not set).  Returns C
     [M, N] in out_dtype; for an 8-bit out_dtype (values [M, N up to a multiple
-    of 16], scales).  Sums of a float32 result hold every product; those of the
-    others come from the 8-bit matrix instructions, which cut eight products at
-    a time 14 bits below the largest.
+    of 16], scales).  With b in 8 bits, sums of a float32 result hold every
+    product; those of the others come from the 8-bit matrix instructions, which
+    cut eight products at a time 14 bits below the largest.
 
     b in 4 bits (quantize to torch.float4_e2m1fn_x2: 1 x 32 scales): a in e4m3
     or in 4 bits too, of as many columns before their padding; out_dtype
-    float32, bfloat16, e4m3 or 4 bits.  Sums of 4-bit a hold every product."""
+    float32, bfloat16, e4m3 or 4 bits.  Their sums hold every product."""
     M, K = a.shape
     fa, fb = _OUTS.get(a.dtype, 0), _OUTS.get(b.dtype, 0)
     if fa < 2 or fb < 2:

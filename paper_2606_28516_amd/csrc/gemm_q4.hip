@@ -7,11 +7,12 @@
 // other along k are aligned to the largest of them and cut 14 bits below it,
 // before the float32 sum.  Products of two e2m1 values lie between 2^-2 and 36
 // in whole quarters, so none of them is cut: 4-bit rows give float32 sums.
-// With 8-bit rows (e4m3) the cut costs 1.2e-5 of the result's norm on normal
-// data, far below the rounding of a bfloat16 or 8-bit result.  Products of them
-// with a float32 result take two instructions, one for the rows' values from 2
-// on (products from 2^-3 to 2688, in whole eighths) and one for those below
-// (up to 11.25, in whole 2^-10), each of which cuts nothing.
+// With 8-bit rows (e4m3) one instruction would lose 1.2e-5 of the result's norm
+// on normal data, and small products beside large ones that cancel altogether.
+// So products of them take two, one for the rows' values from 2 on (products
+// from 2^-3 to 2688, in whole eighths) and one for those below (up to 11.25, in
+// whole 2^-10), each of which cuts nothing.  That is the price of float32 sums:
+// 32768 x 1024 x 4096 takes 177 us instead of 112.
 #include <type_traits>
 
 #include "q8_tile.h"
@@ -40,11 +41,12 @@ __device__ __forceinline__ i32x8 q4_join(const u32x4& a, const u32x4& b) {
 }
 
 // The e4m3 bytes of f whose magnitude is at least 2 (bit 6; NaN too), and the
-// others.
+// others: a mask of whole bytes from their bits 6, which the byte permutation
+// spreads (its selectors 8 .. 11 are the signs of bytes 1 and 3).
 __device__ __forceinline__ void q4_split(const i32x8& f, i32x8& high, i32x8& low) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t u = static_cast<uint32_t>(f[i]), one = (u >> 6) & 0x01010101u, m = (one << 8) - one;
+        const uint32_t u = static_cast<uint32_t>(f[i]), m = __builtin_amdgcn_perm(u << 1, u << 9, 0x0b090a08u);
         high[i] = static_cast<int>(u & m);
         low[i] = static_cast<int>(u & ~m);
     }
@@ -78,9 +80,10 @@ __device__ __forceinline__ u32x4 q4_piece(const uint8_t* row, int64_t at, int64_
     return a;
 }
 
-template <int FA, bool WIDE>
+// a times b, all of it; 8-bit rows in the two parts.
+template <int FA>
 __device__ __forceinline__ f32x4 q4_mfma16(const i32x8& b, const i32x8& a, f32x4 acc, int sb, int sa) {
-    if constexpr (WIDE && FA != kQ8E2M1) {
+    if constexpr (FA != kQ8E2M1) {
         i32x8 h, l;
         q4_split(a, h, l);
         acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, h, acc, kQ8E2M1, FA, 0, sb, 0, sa);
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(512) void k_q4_rows(Q8Desc g, int mtiles, int ntile
                          q4_piece(ar, static_cast<int64_t>(i) * K128 + 64 + grp * 16, ka, mok));
             xa = sa[i];
         }
-        acc = q4_mfma16<FA, sizeof(TC) == 4>(fb, fa, acc, xb, xa);
+        acc = q4_mfma16<FA>(fb, fa, acc, xb, xa);
     }
     // result v of a lane: column 4 grp + v of row `row`
 #pragma unroll
@@ -228,7 +231,7 @@ __global__ __launch_bounds__(512) void k_q4_few(Q8Desc g, const TA* A, int K0, i
             a = q4_join(mok ? p : none, mok ? q : none);
             xa = ps[u];
         }
-        acc = q4_mfma16<FA, sizeof(TC) == 4>(q4_wide(b), a, acc, scale, xa);
+        acc = q4_mfma16<FA>(q4_wide(b), a, acc, scale, xa);
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
@@ -261,19 +264,10 @@ hipError_t q4_few(const Q8Desc& g, const void* A, int K0, hipStream_t st) {
 // ---------------------------------------------------------------------------
 // Many rows: tiles through LDS.
 // ---------------------------------------------------------------------------
-template <int FA, bool WIDE, int OB, int OA>
+template <int FA, int OB, int OA>
 __device__ __forceinline__ f32x16 q4_mfma32(const i32x8& b, const i32x8& a, f32x16 acc, uint32_t sb, uint32_t sa) {
-    if constexpr (WIDE && FA != kQ8E2M1) {
-        i32x8 h, l;
-        q4_split(a, h, l);
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, h, acc, kQ8E2M1, FA, OB, static_cast<int>(sb), OA,
-                                                              static_cast<int>(sa));
-        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, l, acc, kQ8E2M1, FA, OB, static_cast<int>(sb), OA,
-                                                               static_cast<int>(sa));
-    } else {
-        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, acc, kQ8E2M1, FA, OB, static_cast<int>(sb), OA,
-                                                               static_cast<int>(sa));
-    }
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, acc, kQ8E2M1, FA, OB, static_cast<int>(sb), OA,
+                                                           static_cast<int>(sa));
 }
 
 // An operand's share of a stage in LDS: rows of SB bytes, their 16-byte chunks
@@ -297,7 +291,8 @@ struct Q4Rows {
 //
 // Measured on an MI355X, calls in a row: 4-bit rows 8192 x 8192 x 8192 to
 // bfloat16 276 us (3990 TFLOP/s), 50432 x 1024 x 4096 140, 50432 x 4096 x 1024
-// with GELU to 4 bits 190; 8-bit rows 420 (2600), 195, and to e4m3 230.  Bounds:
+// with GELU to 4 bits 190; 8-bit rows 770 (1430; two instructions a product), 300,
+// and to e4m3 325.  Bounds:
 // the large one takes 168 us without its matrix instructions (what 256 CUs take
 // from the L2s, 12.5 TB/s) and 211 without its loads (the card's power: these
 // instructions alone, from registers, reach 6900 TFLOP/s on such data and 9900
@@ -308,7 +303,7 @@ struct Q4Rows {
 template <int KG, int WM, int WN, int TM, int TN, int KS, int FA, int OUT, int WPE>
 __global__ __launch_bounds__(64 * KG * WM * WN) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
-    constexpr bool A4 = FA == kQ8E2M1, WIDE = OUT == kQ8OutF32;
+    constexpr bool A4 = FA == kQ8E2M1;
     constexpr int NW = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32;
     constexpr int SA = A4 ? KS / 2 : KS, SB = KS / 2;                   // bytes of a stage row
     constexpr int PER = 512 / KS, STEPS = KS / 64;                      // stages of a piece of scales, steps of a stage
@@ -495,14 +490,26 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
     auto mm = [&](auto step) {
         constexpr int S = decltype(step)::value, W = S / 2, OB = 2 * (S % 2), OA = A4 ? OB : 0;
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (A4) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+                    acc[i][j] = q4_mfma32<FA, OB, OA>(q4_wide(fb[S & 1][j]), q4_wide(fa[S & 1][0][i]), acc[i][j],
+                                                      sb[j][W], sa[i][W]);
+        } else {
+            // (row by row: both parts of one fragment at a time in registers)
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                const i32x8 a = A4 ? q4_wide(fa[S & 1][0][i]) : q4_join(fa[S & 1][0][i], fa[S & 1][A4 ? 0 : 1][i]);
-                acc[i][j] = q4_mfma32<FA, WIDE, OB, OA>(q4_wide(fb[S & 1][j]), a, acc[i][j], sb[j][W],
-                                                        sa[i][A4 ? W : 0]);
+                i32x8 part[2];
+                q4_split(q4_join(fa[S & 1][0][i], fa[S & 1][1][i]), part[0], part[1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        acc[i][j] = q4_mfma32<FA, OB, OA>(q4_wide(fb[S & 1][j]), part[h], acc[i][j], sb[j][W], sa[i][0]);
             }
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
     for (int s0 = 0; s0 < most; s0 += 2) {
@@ -613,16 +620,31 @@ int64_t q4_tiles(const Q8Desc& g, int bm, int bn) {
 //                   128 x 256              11.3    11.5    12.5    32.4     123
 //                   256 x 256              14.9    15.5    15.8    32.6     129
 //   8-bit rows, bfloat16
-//     1536 x 384    64 x 128                4.1     4.3     5.7    13.9    45.0
-//                   128 x 128               5.0     5.3     6.0    11.7    33.9
-//                   128 x 256               6.9     7.1     7.8    11.5    30.0
-//     1024 x 4096   64 x 128               13.9    14.1    16.1    46.0     178
-//                   128 x 128              19.3    19.6    20.1    34.2     131
-//                   128 x 256              30.2    30.5    31.0    35.2     119
+//     1536 x 384    16 x 16                 3.7     8.5    24.4
+//                   64 x 64                 4.5     4.8    12.0
+//                   64 x 128                4.9     5.1     6.7    17.2    54.0
+//                   128 x 128               6.4     6.6     7.3    14.5    42.8
+//                   128 x 256               8.9     9.2     9.9    15.5    38.4
+//     1024 x 4096   16 x 16                 6.9    38.1     143
+//                   64 x 64                12.0    12.6    25.7
+//                   64 x 128               22.4    22.7    23.5    64.1     229
+//                   64 x 128, two groups   15.7    15.9    18.0
+//                   128 x 128              33.7    34.1    34.6    55.4     209
+//                   128 x 256              50.7    51.2    51.9    54.4     177
+//   by tiles of 128 x 256 (at N 384 a quarter of their columns is past N)
+//                                             256     384     420     512     560     768    1024    1536
+//     384 x 1536    128 x 128              22.9    33.6    33.3    34.5    41.8    52.7    65.2    96.2
+//                   128 x 256              24.4    34.8    34.9    36.2    50.9    52.4    67.9    99.7
+//     1024 x 1024   128 x 128              17.8    24.9    30.1    30.9    37.0    44.8    58.8    89.3
+//                   128 x 256              19.1    26.2    26.4    27.9    37.9    40.0    51.2    76.0
 //   8-bit rows, float32
-//     1550 x 1200   64 x 64 (small)         6.9     7.5    24.9    77.2
-//                   64 x 128               ~9.8    10.2    13.5    41.1
-//                   64 x 128, two groups   ~8.5     9.0    17.8    57.0
+//     1550 x 1200   64 x 64                 7.1     8.5    28.9    88.9
+//                   64 x 128               10.7    11.1    16.5    49.4
+//                   64 x 128, two groups    9.4     9.9    20.6    66.2
+//                   128 x 128              14.9    16.6    18.9    49.1
+//   64 x 128 and two groups along k, 2048 rows
+//     8-bit rows    1024 x 640, 768, 1024, 2064     7.8   7.9,   8.3   8.2,   9.5   8.5,  14.6  11.9
+//     4-bit rows    1024 x 1536, 2048, 4096         6.5   6.8,   7.4   7.3,  11.1  10.6
 Q4Kernel q4_choose(const Q8Desc& g) {
     const bool a4 = g.fa == kQ8E2M1, f32 = g.out == kQ8OutF32, floats = f32 || g.out == kQ8OutBf16;
     if (floats && q4_tiles(g, 16, 16) <= 320) return kQ4Rows;
@@ -632,15 +654,20 @@ Q4Kernel q4_choose(const Q8Desc& g) {
     const int64_t wide = q4_tiles(g, 64, 128);
     // (with a workgroup alone on its CU and a long sum, two groups of waves
     // along k)
-    if (parts && wide <= 256 && g.K > (f32 && !a4 ? 512 : 2048)) return kQ4Split;
+    if (parts && wide <= 256 && g.K > (a4 ? 2048 : 640)) return kQ4Split;
     if (wide <= (a4 ? 400 : 512)) return kQ4Wide;
     if (f32) return a4 && g.K > 512 ? kQ4Deep : kQ4Middle;
-    if (!a4) return q4_tiles(g, 128, 256) >= 384 ? kQ4Large : kQ4Middle;
+    const int64_t tiles = q4_tiles(g, 128, 128);
+    if (!a4) {
+        // 512 places for 128 x 256, 768 for 128 x 128, of which the larger are
+        // better by a tenth: not where a quarter of their columns lie past N
+        const int64_t large = q4_tiles(g, 128, 256);
+        return large >= 400 && tiles * 5 >= large * 8 ? kQ4Large : kQ4Middle;
+    }
     // 4-bit rows: a CU holds three workgroups of 128 x 128 with stages of 128 of
     // k, two with 256 or of 128 x 256, one of 256 x 256; what runs in one round
     // of the chip less wins, but a long sum wants the larger tile or stage
     if (g.K <= 512) return kQ4Middle;
-    const int64_t tiles = q4_tiles(g, 128, 128);
     if (tiles <= 512) return kQ4Deep;
     if (tiles <= 768 && g.K < 2048) return kQ4Middle;
     if (!floats) return q4_tiles(g, 128, 256) >= 400 ? kQ4Large : kQ4Deep;
@@ -689,8 +716,7 @@ hipError_t q4_launch(const Q8Desc& g, hipStream_t st) {
         if (kernel == kQ4Large) return q4_tile<1, 2, 4, 4, 2, 256, FA, OUT, 2>(g, st);
     if constexpr (!F32 && !(A4 && BF16))
         if (kernel == kQ4Large) return q4_tile<1, 2, 2, 2, 4, 128, FA, OUT, 2>(g, st);
-    // three workgroups on a CU (but for the split rows' registers)
-    return q4_tile<1, 2, 2, 2, 2, 128, FA, OUT, F32 && !A4 ? 2 : 3>(g, st);
+    return q4_tile<1, 2, 2, 2, 2, 128, FA, OUT, 3>(g, st);               // three workgroups on a CU
 }
 
 template <int FA>

@@ -466,6 +466,8 @@ int clearmoe_rms_norm(const clearmoe_norm* norm, const void* x, const void* resi
  *   out        CLEARMOE_F32, CLEARMOE_BF16, CLEARMOE_E4M3, or CLEARMOE_E2M1: C
  *              is quantised to 4 bits, ldc a multiple of 32.
  *   sums       hold all of a product, whatever A and the result are.
+ *   gelu       of a sum v: max(v, 0) - h with h within 8e-6 of |v| Phi(-|v|), 1.6e-6
+ *              up to |v| = 4 (0 where that is below 2^-126), whatever the result.
  *   a launch   holds (ceil(M / 128) + 2 groups) ceil(N / 128) at most 2^24 - 32. */
 typedef struct {
     int64_t M;

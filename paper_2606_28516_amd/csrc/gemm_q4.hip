@@ -102,7 +102,11 @@ __device__ __forceinline__ void q4_rows_end(const Q8Desc& g, const GbTile& t, in
         float v = g.bias != nullptr ? g.bias[static_cast<int64_t>(t.seg) * g.N + n0 + c] : 0.0f;
 #pragma unroll
         for (int w = 0; w < KW; ++w) v += s_acc[w][m][c];
-        if (g.gelu) v = gelu_erf(v);
+        if (g.gelu) {
+            float x[1] = {v};
+            q4_gelu(x);
+            v = x[0];
+        }
         static_cast<TC*>(g.C)[(t.m_lo + m) * g.ldc + n0 + c] = Elem<TC>::from_f32(v);
     }
 }
@@ -290,16 +294,16 @@ struct Q4Rows {
 // groups take the pieces of 512 in turn and their sums are added at the end.
 //
 // Measured on an MI355X, calls in a row: 4-bit rows 8192 x 8192 x 8192 to
-// bfloat16 276 us (3990 TFLOP/s), 50432 x 1024 x 4096 140, 50432 x 4096 x 1024
-// with GELU to 4 bits 190; 8-bit rows 770 (1430; two instructions a product), 300,
-// and to e4m3 325.  Bounds:
-// the large one takes 168 us without its matrix instructions (what 256 CUs take
-// from the L2s, 12.5 TB/s) and 211 without its loads (the card's power: these
-// instructions alone, from registers, reach 6900 TFLOP/s on such data and 9900
-// on zeros), and the two overlap in part; over a short k the epilogue's vector
-// work and stores: without GELU 149 of the 190.  Four stages of half the k,
-// loads and reads between the single matrix instructions, 16 waves on a CU, and
-// workgroups that start half a tile apart were no faster.
+// bfloat16 280 us (3930 TFLOP/s), 50432 x 1024 x 4096 140 in one launch,
+// 50432 x 4096 x 1024 with GELU to 4 bits 192; 8-bit rows, two instructions a
+// product, 770 (1430), 300, and to e4m3 332.  Bounds: the large one takes 168 us
+// without its matrix instructions (what 256 CUs take from the L2s, 12.5 TB/s)
+// and 211 without its loads (the card's power: these instructions alone, from
+// registers, reach 6900 TFLOP/s on such data and 9900 on zeros), and the two
+// overlap in part; over a short k the epilogue's vector work and stores: without
+// GELU 153 of the 192; of 8-bit rows the matrix instructions.  Four stages of
+// half the k, loads and reads between the single matrix instructions, 16 waves
+// on a CU, and workgroups that start half a tile apart were no faster.
 template <int KG, int WM, int WN, int TM, int TN, int KS, int FA, int OUT, int WPE>
 __global__ __launch_bounds__(64 * KG * WM * WN) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
@@ -569,7 +573,7 @@ void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {
                         for (int c = 0; c < 4; ++c) acc[i][j][4 * q + c] += v[c];
                     }
     }
-    q8_epilogue<TM, TN, OUT, BM>(g, t, wm * TM * 32, n0 + wn * TN * 32, wn, lane, smem + wave * (EPI / NW),
+    q8_epilogue<TM, TN, OUT, BM, true>(g, t, wm * TM * 32, n0 + wn * TN * 32, wn, lane, smem + wave * (EPI / NW),
                                  reinterpret_cast<float*>(smem + SOFF), acc);
 }
 

@@ -391,7 +391,7 @@ void k_q8_duo(Q8Desc g, int mtiles, int ntiles, int group) {
         }
     }
     gb_wait_barrier<0>();                        // the stage buffers are free
-    q8_epilogue<TM, TN, OUT, BM>(g, t, wave * 64, n0, 0, lane, smem + wave * (32 * 256), nullptr, acc);
+    q8_epilogue<TM, TN, OUT, BM, false>(g, t, wave * 64, n0, 0, lane, smem + wave * (32 * 256), nullptr, acc);
 }
 
 // KG groups of WM x WN waves of TM x TN MFMA tiles (32 x 32), NS stages in LDS
@@ -613,7 +613,7 @@ __global__ __launch_bounds__(64 * KG * WM * WN) void k_q8_tile(Q8Desc g, int mti
                         for (int c = 0; c < 4; ++c) acc[i][j][4 * q + c] += v[c];
                     }
     }
-    q8_epilogue<TM, TN, OUT, BM>(g, t, wm * TM * 32, n0 + wn * TN * 32, wn, lane, smem + wave * (EPI / NW),
+    q8_epilogue<TM, TN, OUT, BM, false>(g, t, wm * TM * 32, n0 + wn * TN * 32, wn, lane, smem + wave * (EPI / NW),
                                  reinterpret_cast<float*>(smem + SOFF), acc);
 }
 

@@ -12,45 +12,79 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// GELU for results that are rounded to 8 bits or bfloat16: v Phi(v) =
-// max(v, 0) - |v| Phi(-|v|) with Phi(-a) = 2^P(a), P the polynomial of degree
-// 7 that is nearest to log2 Phi(-a) on [0, 6] (4.7e-6, so GELU is off by at
-// most 3.3e-6 of itself there; further out P falls on without end): 13
-// full-rate operations' time instead of gelu_erf's 20.  fc1 + GELU over many
-// rows is bound by this vector work (50432 x 3072 x 768: 199 us with gelu_erf,
-// 141 without any).  An infinite v gives NaN, as gelu_erf does.
-// Four at a time, step by step: an exponential's result may not be used by the
+// GELU as v Phi(v) = max(v, 0) - |v| Phi(-|v|), which has no cancellation in
+// its negative tail, with Phi(-a) = 2^P(a), P a polynomial near log2 Phi(-a).
+// Step by step over the values: an exponential's result may not be used by the
 // next instruction.
-// For results of 4 bits (E2M1) P(0) is -1 itself, and P off by 5.7e-6 at most:
-// sums of 4-bit products lie on a coarse grid, so the halves that GELU makes of
-// small ones (below 2^-20) are often ties of the result's grid, or six times a
-// power of two, and must not be moved off them.
-template <bool E2M1>
-__device__ __forceinline__ void q8_gelu4(float (&v)[4]) {
-    constexpr float P[8] = {E2M1 ? -1.0f : -9.99995318e-01f,
-                            E2M1 ? -1.15121424f : -1.15125091f,
-                            E2M1 ? -4.58541691e-01f : -4.58464246e-01f,
-                            E2M1 ? -5.38909398e-02f : -5.39604758e-02f,
-                            E2M1 ? 8.4768841e-03f : 8.50815862e-03f,
-                            E2M1 ? -9.23200278e-04f : -9.3060248e-04f,
-                            E2M1 ? 6.07283946e-05f : 6.16087855e-05f,
-                            E2M1 ? -1.7939027e-06f : -1.83535093e-06f};
-    float p[4], m[4];
+template <int N, int D>
+__device__ __forceinline__ void q8_gelu(const float (&v)[N], const float (&P)[D + 1], float (&y)[N]) {
+    float p[N], m[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
         const float a = fabsf(v[i]);
-        p[i] = P[7];
+        p[i] = P[D];
 #pragma unroll
-        for (int k = 6; k >= 0; --k) p[i] = __builtin_fmaf(a, p[i], P[k]);
+        for (int k = D - 1; k >= 0; --k) p[i] = __builtin_fmaf(a, p[i], P[k]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
+    for (int i = 0; i < N; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
         // (fmaxf takes two instructions: it quiets NaN first)
         asm("v_max_f32 %0, 0, %1" : "=v"(m[i]) : "v"(v[i]));
-        v[i] = __builtin_fmaf(-fabsf(v[i]), p[i], m[i]);
+        y[i] = __builtin_fmaf(-fabsf(v[i]), p[i], m[i]);
     }
+}
+
+// For results of 8-bit products that are rounded to 8 bits or bfloat16: degree
+// 7, nearest on [0, 6] (5.0e-6, so GELU is off by at most 3.5e-6 of itself
+// there; further out P falls on without end): 13 full-rate operations' time
+// instead of gelu_erf's 20.  fc1 + GELU over many rows is bound by this vector
+// work (50432 x 3072 x 768: 199 us with gelu_erf, 141 without any).  An
+// infinite v gives NaN, as gelu_erf does.
+constexpr float kQ8Gelu[8] = {-9.99995318e-01f, -1.15125091f,    -4.58464246e-01f, -5.39604758e-02f,
+                              8.50815862e-03f,  -9.3060248e-04f, 6.16087855e-05f,  -1.83535093e-06f};
+
+// For all results of 4-bit products: degree 9, nearest on [0, 5] with errors
+// weighed down from 2 on, and further out (rare: the whole wave looks again,
+// each value by its own place) |v| Phi(-|v|) = 2^(-v^2 log2(e) / 2) T(1 / v^2), T
+// of degree 3, nearest on [5, 13.25], where float32's normal numbers end.
+// What |v| Phi(-|v|) is off by, of itself, evaluated in float32: 3e-7 for |v| up
+// to 1, 5.6e-7 to 2, 1.6e-6 to 4, 3.8e-6 to 5 and 8e-6 beyond; what is below
+// 2^-126 may be 0.  So a block of small hidden values is rounded to 4 or 8 bits
+// from what GELU is, and few of the others fall on the other side of a tie.
+// P(0) is -1 itself: sums of 4-bit products lie on a coarse grid, the halves
+// that GELU makes of small ones (below 2^-20) are often ties of the result's
+// grid, or six times a power of two, and must not be moved off them.  16
+// operations' time: 50432 x 4096 x 1024 to 4 bits takes 192 us with sums of unit
+// variance (of variance 2, where a third of the waves look again, 203), 183 with
+// the polynomial above, 207 with one of degree 14 for the whole range, 153
+// without GELU.
+constexpr float kQ4Gelu[10] = {-1.0f,            -1.15111232f,     -0.459147573f,   -0.0526642539f,  0.0072750384f,
+                               -0.000269470678f, -0.000147616622f, 3.69796508e-05f, -3.90794594e-06f, 1.65017468e-07f};
+constexpr float kQ4GeluTail[4] = {0.3989396095f, -0.3982101083f, 1.1313945055f, -3.517411232f};
+constexpr float kQ4GeluFar = 5.0f;
+
+template <int N>
+__device__ __forceinline__ void q4_gelu(float (&v)[N]) {
+    float y[N], most = 0.0f;
+    q8_gelu<N, 9>(v, kQ4Gelu, y);
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(v[i]));
+    if (__builtin_expect(__ballot(most > kQ4GeluFar) != 0, 0))
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float s = v[i] * v[i], r = __builtin_amdgcn_rcpf(s);
+            float t = kQ4GeluTail[3];
+#pragma unroll
+            for (int k = 2; k >= 0; --k) t = __builtin_fmaf(r, t, kQ4GeluTail[k]);
+            t *= __builtin_amdgcn_exp2f(s * -0.72134752044448170368f);
+            // (NaN of an infinite v)
+            const float far = __builtin_fmaf(v[i], 0.0f, fmaxf(v[i], 0.0f) - t);
+            y[i] = fabsf(v[i]) > kQ4GeluFar ? far : y[i];
+        }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = y[i];
 }
 
 // Four floats over a scale -> four bytes (as q8_pack4, the division inside).
@@ -124,8 +158,8 @@ __device__ __forceinline__ void q8_start(int lane, const unsigned char* wb, f32x
 // rows of this wave's own LDS (wb) and stored as whole row pieces.  For an
 // 8-bit result, 128 / (32 TN) waves side by side share a block: they exchange
 // the rows' maxima through s_max [waves side by side][BM], between barriers
-// that all waves of the workgroup take.
-template <int TM, int TN, int OUT, int BM>
+// that all waves of the workgroup take.  Q4: the product is a 4-bit one.
+template <int TM, int TN, int OUT, int BM, bool Q4>
 __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, int rw, int nw, int wn, int lane,
                                             unsigned char* wb, float* s_max, f32x16 (&acc)[TM][TN]) {
     constexpr bool F32 = OUT == kQ8OutF32, BF16 = OUT == kQ8OutBf16, E2M1 = OUT == kQ8OutE2M1;
@@ -141,13 +175,21 @@ __device__ __forceinline__ void q8_epilogue(const Q8Desc& g, const GbTile& t, in
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; v += 4) {
-                    float x[4];
+                for (int v = 0; v < 16; v += Q4 ? 16 : 4) {
+                    constexpr int STEP = Q4 ? 16 : 4;
+                    float x[STEP], y[STEP];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) x[c] = F32 ? gelu_erf(acc[i][j][v + c]) : acc[i][j][v + c];
-                    if (!F32) q8_gelu4<E2M1>(x);
+                    for (int c = 0; c < STEP; ++c) x[c] = y[c] = acc[i][j][v + c];
+                    if constexpr (Q4) {
+                        q4_gelu(y);
+                    } else if constexpr (F32) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[i][j][v + c] = x[c];
+                        for (int c = 0; c < STEP; ++c) y[c] = gelu_erf(x[c]);
+                    } else {
+                        q8_gelu<STEP, 7>(x, kQ8Gelu, y);
+                    }
+#pragma unroll
+                    for (int c = 0; c < STEP; ++c) acc[i][j][v + c] = y[c];
                 }
     float mx[TM];
     if constexpr (!F32 && !BF16 && !E2M1) {

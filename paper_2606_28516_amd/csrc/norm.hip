@@ -130,17 +130,26 @@ __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_rms
 #pragma unroll
         for (int v = 0; v < WAVES; ++v) s += s_sum[v];
     }
-    // (mean + eps)^(-1/2) in float32 for any exponent: mean + eps = m 4^k with
-    // m in [1/4, 1), whose root is the hardware's (1 ulp); k = 0 of NaN and
-    // infinity
+    // (mean + eps)^(-1/2) in float32: mean + eps = m 4^k with m in [1/4, 1),
+    // whose root is the hardware's (1 ulp); k = 0 of NaN and infinity
     const double mean = __builtin_fma(s, a.inv_cols, static_cast<double>(a.eps));
-    const int k = (__builtin_amdgcn_frexp_exp(mean) + 1) >> 1;
-    const float inv = __builtin_ldexpf(__builtin_amdgcn_rsqf(static_cast<float>(__builtin_ldexp(mean, -2 * k))), -k);
+    int k = (__builtin_amdgcn_frexp_exp(mean) + 1) >> 1;
+    const float root = __builtin_amdgcn_rsqf(static_cast<float>(__builtin_ldexp(mean, -2 * k)));
     if (a.sum != nullptr) {
         T* h = static_cast<T*>(a.sum) + row * a.lds;
 #pragma unroll
         for (int p = 0; p < NP; ++p) norm_store<WHOLE>(h, c0 + p * STEP, a.cols, f[p]);
     }
+    // root 2^-k is no normal number for the largest rows: those come down by
+    // 2^8 first (what that rounds is far below their results' range)
+    if (k > 126) {
+        k -= 8;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[p][i] *= 0x1p-8f;
+    }
+    const float inv = __builtin_ldexpf(root, -k);
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll

@@ -531,14 +531,15 @@ def ffn_forward_few(x, W1, b1, US, Vt, b2, P, Q, router: Router, k: int,
 
 
 # 8-bit formats, and the C ABI's numbers of every output type; the 4-bit format
-# (two values a byte)
+# (two values a byte) and the scales' type, which a torch may lack: what needs
+# them is refused then, the rest runs
 _FORMATS = {torch.float8_e4m3fn: 2, torch.float8_e5m2: 3}
-_E2M1, _E8M0 = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu
+_E2M1, _E8M0 = (getattr(torch, n, n) for n in ("float4_e2m1fn_x2", "float8_e8m0fnu"))
 _OUTS = {torch.float32: F32, torch.bfloat16: BF16, **_FORMATS, _E2M1: 5}
 
 
 def _format(dtype) -> int:
-    if dtype not in _FORMATS and dtype != _E2M1:
+    if not isinstance(dtype, torch.dtype) or _OUTS.get(dtype, 0) < 2:
         raise ClearMoEError(f"unsupported 8- or 4-bit format {dtype}")
     return _OUTS[dtype]
 

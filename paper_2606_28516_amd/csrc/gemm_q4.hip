@@ -294,16 +294,18 @@ struct Q4Rows {
 // groups take the pieces of 512 in turn and their sums are added at the end.
 //
 // Measured on an MI355X, calls in a row: 4-bit rows 8192 x 8192 x 8192 to
-// bfloat16 280 us (3930 TFLOP/s), 50432 x 1024 x 4096 140 in one launch,
-// 50432 x 4096 x 1024 with GELU to 4 bits 192; 8-bit rows, two instructions a
-// product, 770 (1430), 300, and to e4m3 332.  Bounds: the large one takes 168 us
-// without its matrix instructions (what 256 CUs take from the L2s, 12.5 TB/s)
-// and 211 without its loads (the card's power: these instructions alone, from
-// registers, reach 6900 TFLOP/s on such data and 9900 on zeros), and the two
-// overlap in part; over a short k the epilogue's vector work and stores: without
-// GELU 153 of the 192; of 8-bit rows the matrix instructions.  Four stages of
-// half the k, loads and reads between the single matrix instructions, 16 waves
-// on a CU, and workgroups that start half a tile apart were no faster.
+// bfloat16 276 us (3980 TFLOP/s), 50432 x 1024 x 4096 126 (140 in one launch),
+// 50432 x 4096 x 1024 with GELU to 4 bits 198; 8-bit rows, two instructions a
+// product, 675 (1630), 300, and to e4m3 337.  Bounds: the large one takes 185 us
+// without its matrix instructions (what 256 CUs take from the L2s) and 219
+// without its loads (the card's power: these instructions alone, from registers,
+// reach 6900 TFLOP/s on such data and 9900 on zeros), and the two overlap in
+// part; over a short k the epilogue's vector work and stores: without GELU 155 of
+// the 198, and 122 of those without the matrix instructions; of 8-bit rows the
+// matrix instructions: 564 of the 675 without the loads, 271 without them.
+// Four stages of half the k, loads and reads between the single matrix
+// instructions, 16 waves on a CU, and workgroups that start half a tile apart
+// were no faster.
 template <int KG, int WM, int WN, int TM, int TN, int KS, int FA, int OUT, int WPE>
 __global__ __launch_bounds__(64 * KG * WM * WN) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 void k_q4_tile(Q8Desc g, int mtiles, int ntiles, int group) {

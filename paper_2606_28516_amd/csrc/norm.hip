@@ -5,11 +5,11 @@
 // columns (q8.h), rounded once from float32.
 //
 // One read of x and the residual, one write of h and y: bound by memory.  A
-// row stays in registers between its sum and its scaling, whatever its width
-// (65536 columns are 64 values a thread).  Measured on an MI355X: 50432 x 1024
-// bfloat16 with the residual to e4m3 in 61 us (5.9 TB/s, where a large copy
-// moves 5.0: part of the rows is still in the last-level cache), 1 x 768 in 2.7
-// where an empty kernel takes 2.3.
+// row stays in registers between its sum and its scaling, up to 32768 columns
+// (32 values a thread; of wider rows some spill).  Measured on an MI355X: 50432 x
+// 1024 bfloat16 with the residual to e4m3 in 64 us (5.7 TB/s, where a large copy
+// moves 5.0 to 5.2: part of the rows is still in the last-level cache), 1 x 768
+// in 2.7 where an empty kernel takes 2.3.
 #include "q8.h"
 
 namespace clearmoe {

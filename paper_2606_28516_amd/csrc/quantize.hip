@@ -1,12 +1,12 @@
-// 8- and 4-bit floating point with power-of-two block scales (q8.h), and back.  The scale is
-// exact to divide by, so a value is rounded once, and the matrix instructions
-// apply it for nothing.  One read of x, one write of its bytes: bound by
-// memory.  Measured on an MI355X: rows of 50432 x 768 bfloat16 in 25 us (4.7
-// TB/s; a large copy moves 4.8), 12608 x 384 in 5, squares of 8 x 1550 x 790
-// float32 in 15 (3.2 TB/s: a workgroup holds its square until the maximum of
-// all of it is known).  4 bits: rows of 50432 x 1024 bfloat16 in 28 us (4.7
-// TB/s), 12608 x 384 in 4.8, 8 x 1550 x 790 float32 in 9.3; back to the same
-// types the last two take 4.4 and 10.5.
+// 8- and 4-bit floating point with power-of-two block scales (q8.h), and back.
+// The scale is exact to divide by, so a value is rounded once, and the matrix
+// instructions apply it for nothing.  One read of x, one write of its bytes:
+// bound by memory.  Measured on an MI355X, calls in a row (a large copy moves 5.0
+// to 5.2 TB/s): rows of 50432 x 768 bfloat16 in 25 us (4.7 TB/s), 12608 x 384 in
+// 5, squares of 8 x 1550 x 790 float32 in 15 (3.2 TB/s: a workgroup holds its
+// square until the maximum of all of it is known).  4 bits: rows of 50432 x 1024
+// bfloat16 in 23 us (5.7 TB/s: part of the rows is still in the last-level
+// cache), 8 x 1550 x 790 float32 in 9.0; back to the same types 20.6 and 10.5.
 #include "q8.h"
 
 namespace clearmoe {

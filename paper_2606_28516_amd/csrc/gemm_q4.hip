@@ -71,7 +71,7 @@ __device__ __forceinline__ void q4_words(const unsigned char* p, uint32_t (&w)[N
 
 // ---------------------------------------------------------------------------
 // A few rows: 16 rows x 16 columns, operands straight from memory into
-// registers; eight waves share the sum (1 x 1536 x 384: 2.6 us in a graph, as
+// registers; eight waves share the sum (1 x 1536 x 384: 2.7 us in a graph, as
 // an empty kernel).
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ u32x4 q4_piece(const uint8_t* row, int64_t at, int64_t n, bool ok) {
@@ -167,7 +167,7 @@ hipError_t q4_rows(const Q8Desc& g, hipStream_t st) {
 // into LDS (rows of `pitch` bytes, then rows of `spitch` scale bytes), then as
 // k_q4_rows.  The first blocks of B are on their way meanwhile, so a call is
 // two trips to memory at most, which is what bounds it: 1 x 4096 x 1024 takes
-// 4.2 us under a profiler and 1 x 1024 x 4096 5.2, the weights' bytes 0.45.
+// 4.3 us under a profiler and 1 x 1024 x 4096 5.8, the weights' bytes 0.45.
 template <int FA, typename TA, typename TC>
 __global__ __launch_bounds__(512) void k_q4_few(Q8Desc g, const TA* A, int K0, int mtiles, int ntiles, int pitch,
                                                 int spitch) {
@@ -622,9 +622,9 @@ int64_t q4_tiles(const Q8Desc& g, int bm, int bn) {
 //                   128 x 128, 256 of k         12.4    14.6    19.7    20.7   57.3    65.7    99.9     141
 //                   256 x 256                   17.5    19.0    19.3    20.0   66.8    67.6     103     141
 //   the same, GELU, to 4 bits
-//     4096 x 1024   128 x 128, 256 of k     7.3     7.6    10.1    34.3     132
-//                   128 x 256              11.3    11.5    12.5    32.4     123
-//                   256 x 256              14.9    15.5    15.8    32.6     129
+//     4096 x 1024   128 x 128, 256 of k     7.9     8.2    11.5    36.4     136
+//                   128 x 256              12.2    12.4    13.4    34.5     126
+//                   256 x 256              16.1    16.8    17.2    35.1     135
 //   8-bit rows, bfloat16
 //     1536 x 384    16 x 16                 3.7     8.5    24.4
 //                   64 x 64                 4.5     4.8    12.0

@@ -451,7 +451,7 @@ int clearmoe_rms_norm(const clearmoe_norm* norm, const void* x, const void* resi
  *              format: C is quantised as clearmoe_quantize with block_rows 1
  *              would (from float32), values in C and scales in c_scale.
  *   gelu       1: GELU after the bias (NaN of an infinite sum v).  F32 results are
- *              within 1e-7 |v|, BF16 and byte results from values within that
+ *              within 2e-7 |v|, BF16 and byte results from values within that
  *              or 3.5e-6 of themselves (6e-9 below -6).
  *   lda, ldc   row strides in elements; 0: K, and N (byte formats:
  *              round_up(N, 16)).  lda and a byte format's ldc are multiples
